@@ -544,6 +544,120 @@ int wb_diff2_carry(const wb_field* fields, int32_t n, int32_t pass, int32_t last
                    void* workspace, size_t workspace_bytes, int64_t* index, int64_t* value, int64_t capacity,
                    uint64_t* count, uint64_t* carries, void* stream);
 
+/* ---- operators on a rank's tensors ------------------------------------- */
+
+/* What an MoE layer computes with the tensors a rank holds: the residual norm
+ * in front of it, the router with its balance loss (and their gradient, for
+ * the trainer), the products with plain and with stacked expert weights as
+ * wb_unpack leaves them, and the sum of a token's expert rows.
+ *
+ * Conventions, beside those above:
+ *   - Each call enqueues one or two kernels on `stream` and returns; nothing is
+ *     kept from one call for the next. Calls on different streams may overlap
+ *     when their outputs and workspaces do not.
+ *   - A wb_matrix is rows x cols elements, a row `ld` elements (>= cols) after
+ *     the one before it. Rows and pointers may lie at any multiple of the
+ *     element size (the 16 bytes asked for above do not hold here). At most
+ *     4194303 rows; matrices may have no rows, but have at least one column.
+ *   - Sums, norms, softmax and scales are computed in fp32 and rounded once to
+ *     the output's type, to nearest even. NaN and infinities go through as the
+ *     formulas have it; they stay in their rows.
+ *   - fp8 is E4M3FN. Activations carry one fp32 scale per row and 128 columns,
+ *     [rows, ceil(cols / 128)]: s = max |y| / 448 (1 if that is 0; NaN values
+ *     are left out), q = E4M3(y / s). Weights carry one per 128 x 128 block,
+ *     as wb_unpack writes them with quant_block 128.
+ *   - An output must not overlap an input, except where a call says so. */
+typedef struct wb_matrix {
+  void* data;
+  int32_t dtype;    /* wb_dtype */
+  int32_t reserved;
+  int64_t rows, cols, ld;
+} wb_matrix;
+
+/* total = x + residual; out = total * weight / sqrt(mean(total^2) + eps) over
+ * each row. x, residual and total are WB_F32 or WB_BF16 (each its own), weight
+ * likewise, [1, cols]. residual may be NULL (total = x); total may be NULL
+ * (not written). out is WB_F32, WB_BF16, or WB_F8E4M3 with `scales` (WB_F32,
+ * else NULL). The norm sees the sum before it is rounded to total's type.
+ * total may be x or residual itself. eps >= 0.
+ * Errors: WB_EINVAL (null, shapes that differ, a type not listed), WB_EHIP. */
+int wb_add_rms_norm(const wb_matrix* x, const wb_matrix* residual, const wb_matrix* weight, float eps,
+                    const wb_matrix* total, const wb_matrix* out, const wb_matrix* scales, void* stream);
+
+/* Results of wb_route for T rows, E experts and k choices; device pointers. */
+typedef struct wb_routing {
+  int32_t* experts;   /* [T, k] chosen experts, largest logit first; -1: none */
+  float* gates;       /* [T, k] their weights; 0 where there is none */
+  int32_t* positions; /* [T, k] place of each choice in expert order; -1 where there is none */
+  int32_t* tokens;    /* [T * k] the row at each place; -1 past the last place */
+  int32_t* counts;    /* [E] places of each expert */
+  int32_t* routed;    /* [1] rows that are sent anywhere */
+  int32_t* offsets;   /* [E + 1] first place of each expert; then the number of places */
+  float* loss;        /* [1] balance loss */
+} wb_routing;
+
+/* Send each row of logits [T, E] (WB_F32 or WB_BF16; E <= 1024) to its k
+ * largest (k <= min(E, 64)), ties to the lower expert. p = softmax of the row;
+ * gates are p at the chosen, divided by their sum if `renormalize`. Rows whose
+ * mask byte is 0 (mask may be NULL), and rows without a logit above -inf, are
+ * sent nowhere; -inf is never chosen. Places go by expert, then row. The loss is
+ *   E / (k n^2) sum_e counts_e sum_t p_te   over the n rows that are sent (0 if n is 0).
+ * A NaN or +inf logit makes its row's gates, and the loss, NaN; NaN itself is
+ * not chosen. T * k < 2^31. `workspace`: wb_route_workspace bytes, 16-byte
+ * aligned, free again when the call's work is done.
+ * Errors: WB_EINVAL, WB_EUNSUPPORTED (E or k past the limits), WB_ESIZE, WB_EHIP. */
+int wb_route_workspace(int64_t rows, int32_t experts, size_t* bytes);
+int wb_route(const wb_matrix* logits, const uint8_t* mask, int32_t k, int32_t renormalize, const wb_routing* out,
+             void* workspace, size_t workspace_bytes, void* stream);
+/* Gradient of the logits from those of the gates [T, k] and of the loss [1]
+ * (WB_F32 device pointers, either may be NULL: zero). logits, mask, k and
+ * renormalize as given to wb_route, `routing` what it wrote (experts, gates,
+ * counts and routed are read). d_logits has the logits' type and shape; it may be logits
+ * itself. The choice of experts has no gradient. Errors as wb_route. */
+int wb_route_backward(const wb_matrix* logits, const uint8_t* mask, int32_t k, int32_t renormalize,
+                      const wb_routing* routing, const float* d_gates, const float* d_loss,
+                      const wb_matrix* d_logits, void* stream);
+
+typedef enum wb_activation { WB_ACT_NONE = 0, WB_ACT_SILU = 1, WB_ACT_GELU = 2 } wb_activation; /* gelu: by erf */
+
+/* out = act(x weight^T + bias) + residual, or with `gated`, where the weight is
+ * [gate rows; up rows], act(gate) * up + residual.
+ *   x [T, K], weight [N, K]: both WB_BF16, or both WB_F8E4M3 with x_scales
+ *     [T, ceil(K/128)] and weight_scales [ceil(N/128), ceil(K/128)] (WB_F32;
+ *     else NULL). Sums of 128 products are scaled and added in fp32.
+ *   bias [1, N] (NULL: none), residual [rows, N or N/2] (NULL: none): WB_F32 or WB_BF16.
+ *   out [rows, N or N/2]: WB_F32, WB_BF16, or WB_F8E4M3 with out_scales. It may
+ *     be the residual itself.
+ * With num_experts > 0 the weights are stacked: weight.rows = num_experts * N
+ * rows, weight_scales.rows = num_experts * ceil(N/128), bias [num_experts, N].
+ * offsets [num_experts + 1] (device): row p of out belongs to the expert with
+ * offsets[e] <= p < offsets[e+1]; rows that belong to none are not written
+ * (offsets are clamped to the rows of out). tokens [rows of out] (device, or
+ * NULL): row p comes from row tokens[p] of x (clamped to its rows), else from
+ * row p. Without experts offsets and tokens are NULL, and out has x's rows.
+ * Errors: WB_EINVAL, WB_EUNSUPPORTED (an operand's type, a launch past the
+ * grid's limit), WB_EHIP. */
+typedef struct wb_linear_args {
+  wb_matrix x, x_scales, weight, weight_scales, bias, residual, out, out_scales; /* .data NULL: absent */
+  const int32_t* offsets;
+  const int32_t* tokens;
+  int32_t num_experts;
+  int32_t activation; /* wb_activation */
+  int32_t gated;
+  int32_t reserved;
+} wb_linear_args;
+int wb_linear(const wb_linear_args* args, void* stream);
+
+/* out[t] = residual[t] + sum_i gates[t, i] * y[positions[t, i]], summed in fp32
+ * in the order of i. positions (int32) and gates (WB_F32) are [T, k], 1 <= k
+ * <= 64; places outside y's rows, or outside first[0] <= place < last[0] where
+ * these device pointers are given (a rank's own experts: two entries of
+ * wb_routing.offsets), are left out. residual may be NULL. y, residual and out
+ * are WB_F32 or WB_BF16; out may be the residual itself.
+ * Errors: WB_EINVAL, WB_EUNSUPPORTED (k), WB_EHIP. */
+int wb_combine(const wb_matrix* y, const int32_t* positions, const float* gates, int32_t k, const wb_matrix* residual,
+               const int32_t* first, const int32_t* last, const wb_matrix* out, void* stream);
+
 /* Message of the calling thread's last failed call ("" if none). */
 const char* wb_last_error(void);
 const char* wb_version(void);

@@ -937,3 +937,7 @@ def allocate_locals(layout: Layout, rank: int, device="cuda", zero=False):
         mk = torch.zeros if zero else torch.empty
         out.append(mk(shape, dtype=torch_dtype(lc["dtype"]), device=device))
     return out
+
+
+from .ops import (Routing, add_rms_norm, combine, expert_linear, linear, route,  # noqa: E402,F401
+                  route_backward)

@@ -1,5 +1,5 @@
 """Build libwb.so in-tree: host C++ with g++, gfx950 kernels with hipcc; and
-_args.so, the binding's argument checks (against torch's headers).
+_args.so, the binding's argument checks and its operators' side (against torch's headers).
 
 Run as ``python paper_2609_25442_amd/build.py`` (by path: importing the package
 needs the library). Always recompiles.
@@ -20,8 +20,9 @@ ARGS = os.path.join(HERE, "_args.so")
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 HIPCC = os.path.join(ROCM, "bin", "hipcc")
 
-HOST_SOURCES = ["api.cpp", "layout.cpp", "plan.cpp", "probe.cpp"]
-DEVICE_SOURCES = ["kernels.hip", "probe.hip", "noalloc.hip"]
+HOST_SOURCES = ["api.cpp", "ops_api.cpp", "layout.cpp", "plan.cpp", "probe.cpp"]
+DEVICE_SOURCES = ["kernels.hip", "probe.hip", "noalloc.hip", "norm.hip", "route.hip", "linear.hip"]
+ARGS_SOURCES = ["args.cpp", "args_ops.cpp"]
 # no packed fp32 instructions: hipcc would otherwise form v_pk_*_f32 by itself;
 # a pointer that promises more alignment than its data has is an error, and so is
 # what nothing uses
@@ -48,7 +49,7 @@ def build_args() -> str:
     _run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}", "-isystem", inc, "-isystem",
           os.path.join(inc, "torch", "csrc", "api", "include"), "-isystem", sysconfig.get_paths()["include"],
-          os.path.join(CSRC, "args.cpp"), "-o", ARGS + ".tmp", "-L" + lib, "-ltorch_python", "-ltorch_cpu", "-lc10"])
+          *[os.path.join(CSRC, f) for f in ARGS_SOURCES], "-o", ARGS + ".tmp", "-L" + lib, "-ltorch_python", "-ltorch_cpu", "-lc10"])
     os.replace(ARGS + ".tmp", ARGS)
     return ARGS
 

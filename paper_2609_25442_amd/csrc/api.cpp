@@ -8,34 +8,22 @@
 #include <new>
 #include <string>
 
+#include "entry.hpp"
 #include "wb_internal.hpp"
+
+namespace wb {
+thread_local std::string g_error;
+}
 
 namespace {
 
-thread_local std::string g_error;
-
-int set_error(int code, const std::string& msg) {
-  g_error = msg;
-  return code;
-}
-
-template <class F>
-int guarded(F&& f) {
-  try {
-    g_error.clear();
-    return f();
-  } catch (const wb::Error& e) {
-    return set_error(e.code, e.what());
-  } catch (const std::bad_alloc&) {
-    return set_error(WB_ENOMEM, "host allocation failed");
-  } catch (const std::exception& e) {
-    return set_error(WB_EINVAL, e.what());
-  }
-}
-
-int hip_fail(hipError_t e, const char* what) {
-  return set_error(WB_EHIP, std::string(what) + ": " + hipGetErrorString(e));
-}
+using wb::check_extent;
+using wb::check_extent_as;
+using wb::g_error;
+using wb::guarded;
+using wb::hip_fail;
+using wb::KnownRange;
+using wb::set_error;
 
 int copy_text(const std::string& s, char* buf, size_t cap, size_t* needed) {
   if (needed) *needed = s.size() + 1;
@@ -45,51 +33,6 @@ int copy_text(const std::string& s, char* buf, size_t cap, size_t* needed) {
 }
 
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
-
-// The device allocation of the pointer checked last in one call: the tensors
-// of a rank mostly share a few allocations, and each query of the runtime
-// takes about as long as a launch. Never kept past the call.
-struct KnownRange {
-  uintptr_t begin = 0, end = 0;
-};
-
-// Refuse a pointer the GPU cannot address (pageable host memory, or an
-// address the runtime does not know) and one whose device allocation is
-// smaller than what the kernels will touch. Pinned host memory is accepted;
-// the runtime does not size it. what() names the pointer.
-template <class What>
-int check_extent_as(const void* p, int64_t bytes, What&& what, int align = 16, KnownRange* known = nullptr) {
-  if (!p) return set_error(WB_EINVAL, what() + " is null");
-  if (reinterpret_cast<uintptr_t>(p) % align != 0)
-    return set_error(WB_EINVAL, what() + " is not " + std::to_string(align) + "-byte aligned");
-  const uintptr_t at = reinterpret_cast<uintptr_t>(p);
-  auto fits = [&](uintptr_t end) -> int {
-    if (at + uint64_t(bytes) > end)
-      return set_error(WB_EINVAL, what() + " is smaller than the plan needs (" + std::to_string(bytes) + " bytes)");
-    return WB_OK;
-  };
-  if (known && at >= known->begin && at < known->end) return fits(known->end);
-  hipPointerAttribute_t attr;
-  if (hipPointerGetAttributes(&attr, p) != hipSuccess) {
-    (void)hipGetLastError();
-    return set_error(WB_EINVAL, what() + " is not memory the GPU can address (device or pinned host)");
-  }
-  if (attr.type == hipMemoryTypeUnregistered)
-    return set_error(WB_EINVAL, what() + " is pageable host memory: the kernels need device or pinned host memory");
-  hipDeviceptr_t base = nullptr;
-  size_t size = 0;
-  if (hipMemGetAddressRange(&base, &size, const_cast<void*>(p)) != hipSuccess) {
-    (void)hipGetLastError();
-    return WB_OK;
-  }
-  const uintptr_t begin = reinterpret_cast<uintptr_t>(base);
-  if (known && at >= begin) *known = KnownRange{begin, begin + size};
-  return fits(begin + size);
-}
-
-int check_extent(const void* p, int64_t bytes, const char* what, int align = 16) {
-  return check_extent_as(p, bytes, [&] { return std::string(what); }, align);
-}
 
 // Stage a new pointer table into the workspace when the pointers changed.
 // The device pointer table of `ptrs` for work enqueued on `stream`. A slot

@@ -2,10 +2,13 @@
 // addresses, without a Python call per tensor (a serving rank has hundreds of
 // local tensors, and the checks run on every call). It answers only for plain
 // torch tensors that pass every check; for anything else it says no and the
-// binding's own Python checks decide, with their messages.
+// binding's own Python checks decide, with their messages. The operators'
+// methods are in args_ops.cpp.
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdint>
+
+#include "args_ops.hpp"
 
 namespace {
 
@@ -80,6 +83,11 @@ PyObject* address(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
 PyMethodDef methods[] = {
     {"pointers", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(pointers)), METH_FASTCALL, nullptr},
     {"address", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(address)), METH_FASTCALL, nullptr},
+    {"add_rms_norm", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(wb_py_add_rms_norm)), METH_FASTCALL, nullptr},
+    {"route", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(wb_py_route)), METH_FASTCALL, nullptr},
+    {"route_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(wb_py_route_backward)), METH_FASTCALL, nullptr},
+    {"linear", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(wb_py_linear)), METH_FASTCALL, nullptr},
+    {"combine", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(wb_py_combine)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_args", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
