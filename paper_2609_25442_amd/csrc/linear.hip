@@ -22,6 +22,9 @@ typedef u32x4 u32x4_a1 __attribute__((aligned(1)));
 typedef u32x2 u32x2_a2 __attribute__((aligned(2)));
 typedef uint32_t u32_a1 __attribute__((aligned(1)));
 
+// Read through the scalar cache: the same for the whole wavefront.
+typedef __attribute__((address_space(4))) float ConstFloat;
+
 constexpr int kStageBytes = 128;  // of a row, per step over k: a scale block of fp8, half as many bf16
 
 // Sixteen zero bytes: what a tile's 16-byte pieces past the end of k are read from.
@@ -151,6 +154,32 @@ __device__ __forceinline__ void store_four(void* base, int64_t at, int type, int
   } else {
     for (int r = 0; r < in; ++r) store_one(base, at + r, type, v[r]);
   }
+}
+
+// What follows the sums of a row m and four columns from col on; u are the
+// sums of the up rows where the weight is gated. in_row: columns that exist
+// (none for a row past the end).
+__device__ __forceinline__ void finish(const LinearArgs& a, int expert, int64_t m, int col, int in_row, float (&v)[4],
+                                       float (&u)[4]) {
+  if (a.bias && in_row > 0) {
+    for (int r = 0; r < 4; ++r) {
+      const int c = min(col + r, a.n_out - 1);
+      v[r] += load_bias(a, expert, c);
+      if (a.gated) u[r] += load_bias(a, expert, a.n_out + c);
+    }
+  }
+  for (int r = 0; r < 4; ++r) v[r] = a.gated ? activate(v[r], a.activation) * u[r] : activate(v[r], a.activation);
+  if (a.residual && in_row > 0) {
+    float add[4];
+    load_four(a.residual, m * a.ld_residual + col, a.residual_type, in_row, add);
+    for (int r = 0; r < 4; ++r) v[r] += add[r];
+  }
+}
+
+__device__ __forceinline__ float largest(const float (&v)[4], int in_row, float top) {
+  for (int r = 0; r < 4; ++r)
+    if (r < in_row) top = fmaxf(top, fabsf(v[r]));
+  return top;
 }
 
 // One 16x16 block of sums: the weight's rows down, tokens across (lane l
@@ -382,24 +411,10 @@ __global__ __launch_bounds__(S::kThreads) void wb_linear_tile_kernel(LinearArgs 
       } else {
         for (int r = 0; r < 4; ++r) v[r] = acc[b][j][r], u[r] = 1.0f;
       }
-      if (a.bias && in_row > 0) {
-        for (int r = 0; r < 4; ++r) {
-          const int c = min(col + r, a.n_out - 1);
-          v[r] += load_bias(a, rows.expert, c);
-          if (a.gated) u[r] += load_bias(a, rows.expert, a.n_out + c);
-        }
-      }
-      for (int r = 0; r < 4; ++r) v[r] = a.gated ? activate(v[r], a.activation) * u[r] : activate(v[r], a.activation);
-      if (a.residual && in_row > 0) {
-        float add[4];
-        load_four(a.residual, m * a.ld_residual + col, a.residual_type, in_row, add);
-        for (int r = 0; r < 4; ++r) v[r] += add[r];
-      }
+      finish(a, rows.expert, m, col, in_row, v, u);
       if (a.out_type == WB_F8E4M3) {
-        for (int r = 0; r < 4; ++r) {
-          acc[b][j][r] = v[r];
-          if (r < in_row) top[j] = fmaxf(top[j], fabsf(v[r]));
-        }
+        for (int r = 0; r < 4; ++r) acc[b][j][r] = v[r];
+        top[j] = largest(v, in_row, top[j]);
       } else if (in_row > 0) {
         store_four(a.out, m * a.ld_out + col, a.out_type, in_row, v);
       }
@@ -439,6 +454,211 @@ __global__ __launch_bounds__(S::kThreads) void wb_linear_tile_kernel(LinearArgs 
   }
 }
 
+// Few rows: the weight is read once, so its bytes are the floor. A wavefront
+// takes CB blocks of sixteen rows of the weight (gated: gate and up of the
+// same columns) against NT * 16 tokens and every KS-th stage of k, straight
+// from memory into operands; the KS partial sums meet in LDS and are added in
+// order. FB such groups make a workgroup: eight where the output is fp8, so
+// that it holds the 128 columns of a scale. The sixteen rows of a block share
+// their weight scales (the launch sees to that).
+template <int NT_, int CB_, int FB_, int KS_, bool GATED_>
+struct Few {
+  static constexpr int NT = NT_, CB = CB_, FB = FB_, KS = KS_, kThreads = 64 * FB * KS;
+  static constexpr bool GATED = GATED_;
+  static constexpr int OB = GATED ? 1 : CB, kCols = 16 * OB * FB, kRows = 16 * NT;
+  static constexpr int kItems = (OB * NT + KS - 1) / KS;      // 16x16 blocks a wavefront finishes
+  // stages whose loads are in flight together, as many as the registers hold
+  static constexpr int kAhead = NT + CB <= (kThreads == 1024 ? 2 : 3) ? 4 : 2;
+  static_assert(!GATED || CB == 2, "gate and up");
+};
+
+template <class S, bool F8>
+__global__ __launch_bounds__(S::kThreads) void wb_linear_few_kernel(LinearArgs a, uint32_t tiles_n) {
+  __shared__ f32x4 sums[S::FB * S::KS][S::CB * S::NT][64];
+  __shared__ float tops[S::FB][S::kRows];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int fb = wave / S::KS, ks = wave % S::KS, l15 = lane & 15, quad = lane >> 4;
+  RowTile rows;
+  if (!find_rows(a, blockIdx.x / tiles_n, S::kRows, rows)) return;
+  const int col0 = static_cast<int>(blockIdx.x % tiles_n) * S::kCols + fb * 16 * S::OB;
+  const int64_t k_bytes = F8 ? int64_t(a.k) : 2 * int64_t(a.k);
+  const int whole = static_cast<int>(k_bytes / kStageBytes), stages = static_cast<int>((k_bytes + kStageBytes - 1) / kStageBytes);
+
+  const uint8_t *w[S::CB], *x[S::NT];
+  const ConstFloat* sw[S::CB];
+  const float* sx[S::NT];
+#pragma unroll
+  for (int c = 0; c < S::CB; ++c) {
+    const int first = S::GATED ? c * a.n_out + min(col0, a.n_out - 1) : min(col0 + 16 * c, a.n - 1);
+    const int last = S::GATED ? (c + 1) * a.n_out - 1 : a.n - 1;
+    w[c] = a.weight + rows.expert * a.stride_w_bytes + int64_t(min(first + l15, last)) * a.ld_w_bytes + quad * 16;
+    if constexpr (F8)
+      sw[c] = (const ConstFloat*)(a.weight_scales + rows.expert * a.stride_ws + int64_t(first / kScaleBlock) * a.ld_ws);
+  }
+#pragma unroll
+  for (int j = 0; j < S::NT; ++j) {
+    const int64_t r = x_row(a, min(rows.first + j * 16 + l15, rows.end - 1));
+    x[j] = a.x + r * a.ld_x_bytes + quad * 16;
+    if constexpr (F8) sx[j] = a.x_scales + r * a.ld_xs;
+  }
+
+  f32x4 acc[S::CB][S::NT];
+#pragma unroll
+  for (int c = 0; c < S::CB; ++c)
+#pragma unroll
+    for (int j = 0; j < S::NT; ++j) acc[c][j] = f32x4{0, 0, 0, 0};
+
+  struct Stage {
+    u32x4 w[S::CB][2], x[S::NT][2];
+    float sw[S::CB], sx[S::NT];
+  };
+  auto load = [&](Stage& t, int s) {
+    const int64_t at = int64_t(s) * kStageBytes;
+#pragma unroll
+    for (int c = 0; c < S::CB; ++c) {
+      t.w[c][0] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_a1*>(w[c] + at));
+      t.w[c][1] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_a1*>(w[c] + at + 64));
+      if constexpr (F8) t.sw[c] = sw[c][s];
+    }
+#pragma unroll
+    for (int j = 0; j < S::NT; ++j) {
+      t.x[j][0] = *reinterpret_cast<const u32x4_a1*>(x[j] + at);
+      t.x[j][1] = *reinterpret_cast<const u32x4_a1*>(x[j] + at + 64);
+      if constexpr (F8) t.sx[j] = sx[j][s];
+    }
+  };
+  auto add = [&](const Stage& t) {
+    Operand<F8> xo[S::NT];
+#pragma unroll
+    for (int j = 0; j < S::NT; ++j) xo[j] = Operand<F8>(__builtin_bit_cast(i32x4, t.x[j][0]), __builtin_bit_cast(i32x4, t.x[j][1]));
+#pragma unroll
+    for (int c = 0; c < S::CB; ++c) {
+      const Operand<F8> wo(__builtin_bit_cast(i32x4, t.w[c][0]), __builtin_bit_cast(i32x4, t.w[c][1]));
+#pragma unroll
+      for (int j = 0; j < S::NT; ++j) {
+        if constexpr (F8) {
+          const f32x4 part = block_sum<F8>(wo, xo[j], f32x4{0, 0, 0, 0});
+          const float both = t.sx[j] * t.sw[c];
+          for (int r = 0; r < 4; ++r) acc[c][j][r] = __builtin_fmaf(part[r], both, acc[c][j][r]);
+        } else {
+          acc[c][j] = block_sum<F8>(wo, xo[j], acc[c][j]);
+        }
+      }
+    }
+  };
+  int s = ks;
+  for (; s + (S::kAhead - 1) * S::KS < whole; s += S::kAhead * S::KS) {
+    Stage t[S::kAhead];
+#pragma unroll
+    for (int u = 0; u < S::kAhead; ++u) load(t[u], s + u * S::KS);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int u = 0; u < S::kAhead; ++u) add(t[u]);
+  }
+  for (; s < stages; s += S::KS) {
+    Stage t;
+    if (s < whole) {
+      load(t, s);
+    } else {  // the end of k
+      const int64_t at = int64_t(s) * kStageBytes + quad * 16;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int c = 0; c < S::CB; ++c) t.w[c][h] = load_piece(w[c] - quad * 16, at + 64 * h, k_bytes);
+#pragma unroll
+        for (int j = 0; j < S::NT; ++j) t.x[j][h] = load_piece(x[j] - quad * 16, at + 64 * h, k_bytes);
+      }
+      if constexpr (F8) {
+#pragma unroll
+        for (int c = 0; c < S::CB; ++c) t.sw[c] = sw[c][s];
+#pragma unroll
+        for (int j = 0; j < S::NT; ++j) t.sx[j] = sx[j][s];
+      }
+    }
+    add(t);
+  }
+
+#pragma unroll
+  for (int c = 0; c < S::CB; ++c)
+#pragma unroll
+    for (int j = 0; j < S::NT; ++j) sums[wave][c * S::NT + j][lane] = acc[c][j];
+  __syncthreads();
+  auto total = [&](int c, int j, float(&v)[4]) {
+    f32x4 t = sums[fb * S::KS][c * S::NT + j][lane];
+    for (int i = 1; i < S::KS; ++i) {
+      const f32x4 p = sums[fb * S::KS + i][c * S::NT + j][lane];
+      for (int r = 0; r < 4; ++r) t[r] += p[r];
+    }
+    for (int r = 0; r < 4; ++r) v[r] = t[r];
+  };
+  float v[S::kItems][4];
+#pragma unroll
+  for (int i = 0; i < S::kItems; ++i) {
+    const int item = ks + i * S::KS;
+    if (item >= S::OB * S::NT) break;
+    const int c = item / S::NT, j = item % S::NT, col = col0 + c * 16 + quad * 4;
+    const int64_t m = rows.first + j * 16 + l15;
+    const int in_row = m < rows.end ? a.n_out - col : 0;
+    float u[4] = {1.0f, 1.0f, 1.0f, 1.0f};
+    total(c, j, v[i]);
+    if constexpr (S::GATED) total(1, j, u);
+    finish(a, rows.expert, m, col, in_row, v[i], u);
+    if (a.out_type != WB_F8E4M3) {
+      if (in_row > 0) store_four(a.out, m * a.ld_out + col, a.out_type, in_row, v[i]);
+      continue;
+    }
+    float top = largest(v[i], in_row, 0.0f);
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    if (quad == 0) tops[fb][j * 16 + l15] = top;
+  }
+  if (a.out_type != WB_F8E4M3) return;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < S::kItems; ++i) {
+    const int item = ks + i * S::KS;
+    if (item >= S::OB * S::NT) break;
+    const int j = item % S::NT, col = col0 + quad * 4;
+    const int64_t m = rows.first + j * 16 + l15;
+    const int in_row = m < rows.end ? a.n_out - col : 0;
+    if (in_row <= 0) continue;
+    float most = 0.0f;
+    for (int f = 0; f < S::FB; ++f) most = fmaxf(most, tops[f][j * 16 + l15]);
+    const RowScale q = row_scale(most);
+    if (quad == 0 && fb == 0) a.out_scales[m * a.ld_os + col / kScaleBlock] = q.s;
+    for (int r = 0; r < 4; ++r) v[i][r] = quotient(v[i][r], q);
+    store_four(a.out, m * a.ld_out + col, WB_F8E4M3, in_row, v[i]);
+  }
+}
+
+// Row tiles of `per` rows: each expert's last may be part of one, so there is
+// at most one more per expert with rows.
+int64_t row_tiles(const LinearArgs& a, int per) {
+  if (!a.offsets) return (a.rows + per - 1) / per;
+  return std::min<int64_t>(a.rows, a.rows / per + std::min<int64_t>(a.num_experts, a.rows));
+}
+
+template <class S>
+hipError_t launch_few(const LinearArgs& a, hipStream_t st) {
+  const int64_t tiles_n = (a.n_out + S::kCols - 1) / S::kCols, all = row_tiles(a, S::kRows) * tiles_n;
+  if (all > 0x3fffff) return hipErrorInvalidConfiguration;
+  const dim3 grid(static_cast<uint32_t>(all)), block(S::kThreads);
+  if (a.in_type == WB_F8E4M3)
+    hipLaunchKernelGGL((wb_linear_few_kernel<S, true>), grid, block, 0, st, a, static_cast<uint32_t>(tiles_n));
+  else
+    hipLaunchKernelGGL((wb_linear_few_kernel<S, false>), grid, block, 0, st, a, static_cast<uint32_t>(tiles_n));
+  return hipGetLastError();
+}
+
+// NT * 16 tokens at a time.
+template <int NT>
+hipError_t launch_few_rows(const LinearArgs& a, hipStream_t st) {
+  constexpr int kSplit = NT == 1 ? 2 : 1;  // of k, in the workgroups of eight groups
+  if (a.out_type == WB_F8E4M3)
+    return a.gated ? launch_few<Few<NT, 2, 8, kSplit, true>>(a, st) : launch_few<Few<NT, 1, 8, kSplit, false>>(a, st);
+  return a.gated ? launch_few<Few<NT, 2, 1, 8, true>>(a, st) : launch_few<Few<NT, 1, 1, 8, false>>(a, st);
+}
+
 template <class S, bool F8, bool DIRECT>
 hipError_t launch_tile(const LinearArgs& a, hipStream_t st) {
   const auto kernel = wb_linear_tile_kernel<S, F8, DIRECT>;
@@ -446,11 +666,8 @@ hipError_t launch_tile(const LinearArgs& a, hipStream_t st) {
   if (e != hipSuccess) return e;
   const int step = a.gated ? S::BN / 2 : S::BN;
   const int64_t tiles_n = (a.n_out + step - 1) / step;
-  // each expert's last tile may be part of one: at most one more per expert with rows
-  int64_t tiles_m = (a.rows + S::BM - 1) / S::BM;
-  if (a.offsets) tiles_m = std::min<int64_t>(a.rows, a.rows / S::BM + std::min<int64_t>(a.num_experts, a.rows));
-  const int64_t all = tiles_m * tiles_n;
-  if (all <= 0 || all > 0x3fffff) return all == 0 ? hipSuccess : hipErrorInvalidConfiguration;
+  const int64_t all = row_tiles(a, S::BM) * tiles_n;
+  if (all > 0x3fffff) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>(all)), dim3(S::kThreads), S::kLds, st, a,
                      static_cast<uint32_t>(tiles_n), 8u);
   return hipGetLastError();
@@ -466,7 +683,14 @@ hipError_t launch_shape(const LinearArgs& a, hipStream_t st) {
 
 int launch_linear(const LinearArgs& a, void* stream) {
   if (a.rows == 0) return hipSuccess;
-  return launch_shape<Shape<64, 256, 1, 4>>(a, static_cast<hipStream_t>(stream));
+  const auto st = static_cast<hipStream_t>(stream);
+  const int64_t each = a.offsets ? a.rows / a.num_experts : a.rows;  // rows a weight meets
+  const bool shared_scales = a.in_type != WB_F8E4M3 || !a.gated || a.n_out % 16 == 0;
+  if (!shared_scales) return launch_shape<Shape<64, 256, 1, 4>>(a, st);
+  if (each <= 16) return launch_few_rows<1>(a, st);
+  if (each <= 32) return launch_few_rows<2>(a, st);
+  if (each <= 64) return launch_few_rows<4>(a, st);
+  return launch_shape<Shape<64, 256, 1, 4>>(a, st);
 }
 
 }  // namespace wb
