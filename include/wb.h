@@ -636,7 +636,7 @@ typedef enum wb_activation { WB_ACT_NONE = 0, WB_ACT_SILU = 1, WB_ACT_GELU = 2 }
  * NULL): row p comes from row tokens[p] of x (clamped to its rows), else from
  * row p. Without experts offsets and tokens are NULL, and out has x's rows.
  * Errors: WB_EINVAL, WB_EUNSUPPORTED (an operand's type, a launch past the
- * grid's limit), WB_EHIP. */
+ * grid's limit), WB_ESIZE, WB_EHIP. */
 typedef struct wb_linear_args {
   wb_matrix x, x_scales, weight, weight_scales, bias, residual, out, out_scales; /* .data NULL: absent */
   const int32_t* offsets;
@@ -646,7 +646,12 @@ typedef struct wb_linear_args {
   int32_t gated;
   int32_t reserved;
 } wb_linear_args;
-int wb_linear(const wb_linear_args* args, void* stream);
+/* `workspace` (16-byte aligned, free again when the call's work is done) holds
+ * the fp32 rows of some fp8 results; wb_linear_workspace says how many bytes
+ * the same arguments need, 0 for most (then it may be NULL). Its errors are
+ * those of wb_linear, WB_ESIZE aside. */
+int wb_linear_workspace(const wb_linear_args* args, size_t* bytes);
+int wb_linear(const wb_linear_args* args, void* workspace, size_t workspace_bytes, void* stream);
 
 /* out[t] = residual[t] + sum_i gates[t, i] * y[positions[t, i]], summed in fp32
  * in the order of i. positions (int32) and gates (WB_F32) are [T, k], 1 <= k

@@ -230,23 +230,24 @@ PyObject* wb_py_route_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
   });
 }
 
-// linear(fn, x, weight, offsets, tokens, x_scales, weight_scales, bias, residual, activation, gated, out_dtype, device,
+// linear(fn, workspace_fn, x, weight, offsets, tokens, x_scales, weight_scales, bias, residual, activation, gated, out_dtype, device,
 //        stream) -> out or (out, scales)
 PyObject* wb_py_linear(PyObject*, PyObject* const* args, Py_ssize_t n) {
-  if (!counted(n, 14, "linear")) return nullptr;
+  if (!counted(n, 15, "linear")) return nullptr;
   return guarded([&]() -> PyObject* {
-    const Where at(args + 12);
-    const long activation = PyLong_AsLong(args[9]), gated = PyLong_AsLong(args[10]), type = PyLong_AsLong(args[11]);
+    const Where at(args + 13);
+    const long activation = PyLong_AsLong(args[10]), gated = PyLong_AsLong(args[11]), type = PyLong_AsLong(args[12]);
     auto* fn = function<decltype(wb_linear)>(args[0]);
+    auto* size = function<decltype(wb_linear_workspace)>(args[1]);
     if (PyErr_Occurred()) return nullptr;
-    const Tensor& x = needed(args[1], "x", at.device);
-    const Tensor& weight = needed(args[2], "weight", at.device);
-    const Tensor* offsets = tensor(args[3], "offsets", at.device);
-    const Tensor* tokens = tensor(args[4], "tokens", at.device);
-    const Tensor* x_scales = tensor(args[5], "x_scales", at.device);
-    const Tensor* weight_scales = tensor(args[6], "weight_scales", at.device);
-    const Tensor* bias = tensor(args[7], "bias", at.device);
-    const Tensor* residual = tensor(args[8], "residual", at.device);
+    const Tensor& x = needed(args[2], "x", at.device);
+    const Tensor& weight = needed(args[3], "weight", at.device);
+    const Tensor* offsets = tensor(args[4], "offsets", at.device);
+    const Tensor* tokens = tensor(args[5], "tokens", at.device);
+    const Tensor* x_scales = tensor(args[6], "x_scales", at.device);
+    const Tensor* weight_scales = tensor(args[7], "weight_scales", at.device);
+    const Tensor* bias = tensor(args[8], "bias", at.device);
+    const Tensor* residual = tensor(args[9], "residual", at.device);
     wb_linear_args a{};
     a.x = matrix(x, "x"), a.weight = matrix(weight, "weight", offsets != nullptr);
     a.activation = static_cast<int32_t>(activation), a.gated = gated != 0;
@@ -272,8 +273,15 @@ PyObject* wb_py_linear(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const at::ScalarType t = type_of(static_cast<int32_t>(type));
     Tensor out = fresh({rows, cols}, t, x), scales;
     a.out = matrix(out, "out");
-    if (t == at::kFloat8_e4m3fn) scales = fresh({rows, scale_cols(cols)}, at::kFloat, x), a.out_scales = matrix(scales, "scales");
-    const int rc = fn(&a, at.stream);
+    Tensor workspace;
+    size_t bytes = 0;
+    int rc = WB_OK;
+    if (t == at::kFloat8_e4m3fn) {  // only these may need one
+      scales = fresh({rows, scale_cols(cols)}, at::kFloat, x), a.out_scales = matrix(scales, "scales");
+      rc = size(&a, &bytes);
+      if (rc == WB_OK && bytes) workspace = fresh({static_cast<int64_t>(bytes)}, at::kByte, x);
+    }
+    if (rc == WB_OK) rc = fn(&a, bytes ? workspace.data_ptr() : nullptr, bytes, at.stream);
     if (rc != WB_OK) return PyLong_FromLong(rc);
     if (!scales.defined()) return wrap(out);
     return Py_BuildValue("(NN)", wrap(out), wrap(scales));

@@ -10,6 +10,7 @@
 // fp8 codes are widened to bf16 (exactly) on their way to the matrix cores;
 // the sums of a block are scaled and added in fp32.
 #include <algorithm>
+#include <cmath>
 
 #include "ops_device.hpp"
 
@@ -21,9 +22,6 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef u32x4 u32x4_a1 __attribute__((aligned(1)));
 typedef u32x2 u32x2_a2 __attribute__((aligned(2)));
 typedef uint32_t u32_a1 __attribute__((aligned(1)));
-
-// Read through the scalar cache: the same for the whole wavefront.
-typedef __attribute__((address_space(4))) float ConstFloat;
 
 constexpr int kStageBytes = 128;  // of a row, per step over k: a scale block of fp8, half as many bf16
 
@@ -219,18 +217,24 @@ __device__ __forceinline__ f32x4 block_sum(const Operand<F8>& w, const Operand<F
 }
 
 // A workgroup's tile: BM rows of the output by BN rows of the weight, WM x WN
-// wavefronts. LDS holds two stages of 128 bytes of every row of both; the
-// pieces of a row are permuted by its number so that sixteen rows' pieces at
-// one place of k fall into different banks.
-template <int BM_, int BN_, int WM_, int WN_>
+// wavefronts. LDS holds a ring of RING slots of STEP stages of every row of
+// both; a barrier stands between slots, so small tiles take more stages at
+// once, and KG such sets of wavefronts share them out (their sums meet in LDS
+// at the end, in order). The pieces of a row are permuted by its number so that sixteen rows'
+// pieces at one place of k fall into different banks.
+template <int BM_, int BN_, int WM_, int WN_, int KG_, int STEP_, int RING_>
 struct Shape {
-  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
-  static constexpr int kThreads = 64 * WM * WN, TM = BM / WM, TN = BN / WN, FM = TM / 16, FN = TN / 16;
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, KG = KG_, STEP = STEP_, RING = RING_;
+  static constexpr int kThreads = 64 * WM * WN * KG, TM = BM / WM, TN = BN / WN, FM = TM / 16, FN = TN / 16;
   static constexpr int kRows = BM + BN, kStage = kRows * kStageBytes;
-  // behind the stages: scales of x by row and of the weight by row, for each
-  // of the two; the epilogue's maxima lie over them
-  static constexpr int kScales = (BM + BN) * 4, kLds = 2 * kStage + 2 * kScales;
-  static_assert(WN * BM * 4 <= 2 * kScales, "maxima fit");
+  // behind the slots: for each, the scales of its stages' rows, of x and then
+  // of the weight; the epilogue's maxima lie over them
+  static constexpr int kSlot = STEP * kStage, kRounds = (STEP * kRows + kThreads - 1) / kThreads;
+  static constexpr int kScales = kRounds * kThreads * 4, kLds = RING * (kSlot + kScales);
+  static_assert(kLds <= 160 * 1024, "");
+  static_assert(WN * BM * 4 <= RING * kScales, "maxima fit");
+  static_assert((KG - 1) * BM * BN * 4 <= RING * kSlot, "the ring holds the groups' sums");
+  static_assert(kRows * STEP * 8 % kThreads == 0 && kRows % 16 == 0 && STEP % KG == 0, "the pieces share out evenly");
 };
 
 __device__ __forceinline__ int swizzle(int row) { return (row >> 1) & 7; }
@@ -243,7 +247,8 @@ template <class S, bool F8, bool DIRECT>
 __global__ __launch_bounds__(S::kThreads) void wb_linear_tile_kernel(LinearArgs a, uint32_t tiles_n, uint32_t group) {
   extern __shared__ __align__(128) uint8_t lds[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wm = wave / S::WN, wn = wave % S::WN, l15 = lane & 15, quad = lane >> 4;
+  const int kg = wave / (S::WM * S::WN), wm = wave / S::WN % S::WM, wn = wave % S::WN;
+  const int l15 = lane & 15, quad = lane >> 4;
 
   // tiles of `group` neighbouring row tiles side by side, so that the rows of
   // the weight they share are read while they are in cache; neighbouring
@@ -266,69 +271,88 @@ __global__ __launch_bounds__(S::kThreads) void wb_linear_tile_kernel(LinearArgs 
     return r < S::BN ? weight + int64_t(w_row(a, col0, r)) * a.ld_w_bytes
                      : a.x + x_row(a, min(rows.first + (r - S::BN), rows.end - 1)) * a.ld_x_bytes;
   };
-  constexpr int kPieces = S::kRows * 8 / S::kThreads;  // per lane and stage
+  constexpr int kWaves = S::kThreads / 64, kPieces = S::kRows * S::STEP * 8 / S::kThreads;  // per lane and step
+  static_assert(kWaves % 2 == 0, "the pieces of a lane are permuted alike");
+  const int piece = ((lane & 7) ^ swizzle(wave * 8 + (lane >> 3))) * 16;
   const uint8_t* src[kPieces];
   u32x4 held[DIRECT ? 1 : kPieces];
 #pragma unroll
   for (int i = 0; i < kPieces; ++i) {
-    const int r = (wave + i * (S::kThreads / 64)) * 8 + (lane >> 3);
-    src[i] = row_of(r);
+    const int r = (wave + i * kWaves) * 8;  // of the step's rows; its stage is the same for the wavefront
+    src[i] = row_of(r % S::kRows + (lane >> 3)) + r / S::kRows * kStageBytes;
   }
-  const int r0 = wave * 8 + (lane >> 3);
-  static_assert((S::kThreads / 64 * 8) % 16 == 0, "the pieces of a lane are permuted alike");
-  const int piece = ((lane & 7) ^ swizzle(r0)) * 16;
-
-  auto fetch = [&](int s) {
-    const int64_t at = int64_t(s) * kStageBytes + piece;
-    if constexpr (DIRECT) {
-      uint8_t* to = lds + (s & 1) * S::kStage;
-      const bool past = at >= k_bytes;
-#pragma unroll
-      for (int i = 0; i < kPieces; ++i) {
-        const uint8_t* p = past ? reinterpret_cast<const uint8_t*>(&zero_piece) : src[i] + at;
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p,
-                                         (__attribute__((address_space(3))) void*)(to + (wave + i * (S::kThreads / 64)) * 1024),
-                                         16, 0, 0);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < kPieces; ++i) held[i] = load_piece(src[i], at, k_bytes);
-    }
-  };
-  auto put = [&](int s) {
-    if constexpr (!DIRECT) {
-      uint8_t* to = lds + (s & 1) * S::kStage;
-#pragma unroll
-      for (int i = 0; i < kPieces; ++i)
-        *reinterpret_cast<u32x4*>(to + (wave + i * (S::kThreads / 64)) * 1024 + lane * 16) = held[i];
-    }
-  };
-
-  // scales of a stage, one row (of x, then of the weight) per thread and round
-  constexpr int kScaleRows = F8 ? S::BM + S::BN : 0, kScaleRounds = (kScaleRows + S::kThreads - 1) / S::kThreads;
-  const float* scale_src[kScaleRounds > 0 ? kScaleRounds : 1];
-  float scale_held[kScaleRounds > 0 ? kScaleRounds : 1];
-  float* const scales = reinterpret_cast<float*>(lds + 2 * S::kStage);
+  // scales: a row of x, then of the weight, per thread and round
+  const float* scale_src[S::kRounds];
+  float scale_held[S::kRounds];
+  uint8_t* const scales = lds + S::RING * S::kSlot;
   if constexpr (F8) {
 #pragma unroll
-    for (int i = 0; i < kScaleRounds; ++i) {
-      const int r = tid + i * S::kThreads;
+    for (int i = 0; i < S::kRounds; ++i) {
+      const int g = min(tid + i * S::kThreads, S::STEP * S::kRows - 1), r = g % S::kRows;
       scale_src[i] = r < S::BM ? a.x_scales + x_row(a, min(rows.first + r, rows.end - 1)) * a.ld_xs
                                : a.weight_scales + rows.expert * a.stride_ws +
-                                     int64_t(w_row(a, col0, min(r, kScaleRows - 1) - S::BM) / kScaleBlock) * a.ld_ws;
+                                     int64_t(w_row(a, col0, r - S::BM) / kScaleBlock) * a.ld_ws;
     }
   }
-  auto fetch_scales = [&](int s) {
+
+  // start step t's stages on their way into a slot of the ring: DIRECT, all
+  // the way. Stages past the end are zeros.
+  int put_at = 0;
+  auto fetch = [&](int t, int slot) {
+    put_at = slot;
+    const int64_t at = int64_t(t) * (S::STEP * kStageBytes) + piece;
+    const bool whole = (t + 1) * int64_t(S::STEP * kStageBytes) <= k_bytes;
     if constexpr (F8) {
 #pragma unroll
-      for (int i = 0; i < kScaleRounds; ++i) scale_held[i] = scale_src[i][s];
+      for (int i = 0; i < S::kRounds; ++i) {
+        const int h = min(tid + i * S::kThreads, S::STEP * S::kRows - 1) / S::kRows;
+        const float* p = scale_src[i] + min(t * S::STEP + h, stages - 1);
+        if constexpr (DIRECT)
+          __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p,
+                                           (__attribute__((address_space(3))) void*)(scales + slot * S::kScales + (wave * 64 + i * S::kThreads) * 4),
+                                           4, 0, 0);
+        else
+          scale_held[i] = *p;
+      }
+    }
+    if constexpr (DIRECT) {
+      uint8_t* to = lds + slot * S::kSlot + wave * 1024;
+      auto load = [&](const uint8_t* p, int i) {
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p,
+                                         (__attribute__((address_space(3))) void*)(to + i * kWaves * 1024), 16, 0, 0);
+      };
+      if (whole) {
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) load(src[i] + at, i);
+      } else {
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+          const int64_t from = at + (wave + i * kWaves) * 8 / S::kRows * kStageBytes;
+          load(from < k_bytes ? src[i] + at : reinterpret_cast<const uint8_t*>(&zero_piece), i);
+        }
+      }
+    } else if (whole) {
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i) held[i] = *reinterpret_cast<const u32x4_a1*>(src[i] + at);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i) {
+        const int stage = (wave + i * kWaves) * 8 / S::kRows * kStageBytes;
+        held[i] = load_piece(src[i] - stage, at + stage, k_bytes);
+      }
     }
   };
-  auto put_scales = [&](int s) {
-    if constexpr (F8) {
+  // not DIRECT: what fetch() left in registers goes into its slot
+  auto put = [&]() {
+    if constexpr (!DIRECT) {
+      uint8_t* to = lds + put_at * S::kSlot + wave * 1024 + lane * 16;
 #pragma unroll
-      for (int i = 0; i < kScaleRounds; ++i)
-        if (tid + i * S::kThreads < kScaleRows) scales[(s & 1) * kScaleRows + tid + i * S::kThreads] = scale_held[i];
+      for (int i = 0; i < kPieces; ++i) *reinterpret_cast<u32x4*>(to + i * kWaves * 1024) = held[i];
+      if constexpr (F8) {
+#pragma unroll
+        for (int i = 0; i < S::kRounds; ++i)
+          *reinterpret_cast<float*>(scales + put_at * S::kScales + (tid + i * S::kThreads) * 4) = scale_held[i];
+      }
     }
   };
 
@@ -341,19 +365,27 @@ __global__ __launch_bounds__(S::kThreads) void wb_linear_tile_kernel(LinearArgs 
   const int frag = l15 * kStageBytes + ((quad ^ swizzle(l15)) << 4);
   const int w_frag = wn * S::TN * kStageBytes + frag, x_frag = (S::BN + wm * S::TM) * kStageBytes + frag;
 
-  fetch_scales(0);
-  fetch(0);
-  put(0);
-  put_scales(0);
-  for (int s = 0; s < stages; ++s) {
-    // this stage is in LDS, and the one before it has been read
-    __syncthreads();
-    if (s + 1 < stages) {
-      fetch_scales(s + 1);
-      fetch(s + 1);
-    }
-    const uint8_t* buf = lds + (s & 1) * S::kStage;
-    const float* sc = scales + (s & 1) * kScaleRows;
+  // DIRECT keeps RING - 1 steps in flight, the other way one
+  constexpr int kAhead = DIRECT ? S::RING - 1 : 1;
+  constexpr int kLoads = kPieces + (F8 ? S::kRounds : 0);  // of a wavefront and step
+  static_assert(!DIRECT || (kAhead - 1) * kLoads < 64, "the counter of loads in flight");
+  const int steps = (stages + S::STEP - 1) / S::STEP;
+  for (int t = 0; t < min(kAhead, steps); ++t) fetch(t, t);
+  put();
+  int slot = 0;
+  for (int t = 0; t < steps; ++t) {
+    // after this, step t is in LDS for every wavefront, and the step before it
+    // has been read by all: its slot can be filled
+    if (DIRECT && t + kAhead <= steps)
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((kAhead - 1) * kLoads) : "memory");
+    else
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (t + kAhead < steps) fetch(t + kAhead, slot + kAhead >= S::RING ? slot + kAhead - S::RING : slot + kAhead);
+#pragma unroll
+    for (int h = 0; h < S::STEP / S::KG; ++h) {
+    const int stage = h * S::KG + kg;
+    const uint8_t* buf = lds + slot * S::kSlot + stage * S::kStage;
+    const float* sc = reinterpret_cast<const float*>(scales + slot * S::kScales) + stage * S::kRows;
     auto operand = [&](int at) {
       return Operand<F8>(*reinterpret_cast<const i32x4*>(buf + at), *reinterpret_cast<const i32x4*>(buf + (at ^ 64)));
     };
@@ -385,249 +417,118 @@ __global__ __launch_bounds__(S::kThreads) void wb_linear_tile_kernel(LinearArgs 
         for (int j = 0; j < S::FM; ++j) acc[i][j] = block_sum<F8>(w, x[j], acc[i][j]);
       }
     }
-    if (s + 1 < stages) {
-      put(s + 1);
-      put_scales(s + 1);
+    }
+    slot = slot + 1 == S::RING ? 0 : slot + 1;
+    if (t + 1 < steps) put();
+  }
+
+  if constexpr (S::KG > 1) {
+    float* const sums = reinterpret_cast<float*>(lds);
+    const int own = (wave % (S::WM * S::WN) * S::FN * S::FM) * 256 + lane * 4;
+    __syncthreads();
+    if (kg > 0) {
+#pragma unroll
+      for (int i = 0; i < S::FN; ++i)
+#pragma unroll
+        for (int j = 0; j < S::FM; ++j)
+          *reinterpret_cast<f32x4*>(sums + (kg - 1) * S::BM * S::BN + own + (i * S::FM + j) * 256) = acc[i][j];
+    }
+    __syncthreads();
+    if (kg == 0) {
+#pragma unroll
+      for (int i = 0; i < S::FN; ++i)
+#pragma unroll
+        for (int j = 0; j < S::FM; ++j)
+          for (int g = 0; g < S::KG - 1; ++g) {
+            const f32x4 add = *reinterpret_cast<const f32x4*>(sums + g * S::BM * S::BN + own + (i * S::FM + j) * 256);
+            for (int r = 0; r < 4; ++r) acc[i][j][r] += add[r];
+          }
     }
   }
 
-  // epilogue: lane l holds token l % 16 of each j, four columns of each block.
-  // A gated tile's blocks come in pairs, gate and up of the same columns.
-  const int blocks = a.gated ? S::FN / 2 : S::FN;
-  const int wave_col = col0 + wn * (a.gated ? S::TN / 2 : S::TN) + quad * 4;
-  float top[S::FM];
+  // epilogue, sixteen rows at a time through LDS: a wavefront puts its sums
+  // down by row and takes them up again four neighbouring columns per lane, a
+  // row by neighbouring lanes, which is also how they are stored
+  constexpr int kPitch = S::TN + 4;  // floats
+  static_assert(S::WM * S::WN * 16 * kPitch * 4 <= S::RING * S::kSlot, "the ring holds the sums");
+  float* const mine = reinterpret_cast<float*>(lds) + wave % (S::WM * S::WN) * 16 * kPitch;
+  float* const tops = reinterpret_cast<float*>(scales);
+  const int cols = a.gated ? S::TN / 2 : S::TN, lanes = cols / 4, span = kScaleBlock / cols;
+  const int wave_col = col0 + wn * cols, c = lane % lanes * 4, per = 64 / lanes;
+  const int at = a.gated ? (c >> 4) * 32 + (c & 15) : c;
+  const int in_row = a.n_out - (wave_col + c), first_r = kg == 0 ? lane / lanes : 16;
+  const bool f8_out = a.out_type == WB_F8E4M3;
+  __syncthreads();
 #pragma unroll
   for (int j = 0; j < S::FM; ++j) {
-    const int64_t m = rows.first + wm * S::TM + j * 16 + l15;
-    const bool there = m < rows.end;
-    top[j] = 0.0f;
+    if (kg == 0) {
 #pragma unroll
-    for (int b = 0; b < S::FN; ++b) {
-      if (b >= blocks) break;
-      const int col = wave_col + b * 16, in_row = there ? a.n_out - col : 0;
-      float v[4], u[4];
-      if (a.gated) {
-        for (int r = 0; r < 4; ++r) v[r] = acc[2 * b < S::FN ? 2 * b : 0][j][r], u[r] = acc[2 * b + 1 < S::FN ? 2 * b + 1 : 0][j][r];
-      } else {
-        for (int r = 0; r < 4; ++r) v[r] = acc[b][j][r], u[r] = 1.0f;
-      }
-      finish(a, rows.expert, m, col, in_row, v, u);
-      if (a.out_type == WB_F8E4M3) {
-        for (int r = 0; r < 4; ++r) acc[b][j][r] = v[r];
-        top[j] = largest(v, in_row, top[j]);
-      } else if (in_row > 0) {
-        store_four(a.out, m * a.ld_out + col, a.out_type, in_row, v);
+      for (int i = 0; i < S::FN; ++i) *reinterpret_cast<f32x4*>(mine + l15 * kPitch + i * 16 + quad * 4) = acc[i][j];
+    }
+#pragma unroll 1
+    for (int r = first_r; r < 16; r += per) {
+      const int64_t m = rows.first + wm * S::TM + j * 16 + r;
+      const int in = m < rows.end ? in_row : 0;
+      float* p = mine + r * kPitch + at;
+      const f32x4 g = *reinterpret_cast<const f32x4*>(p);
+      const f32x4 w = a.gated ? *reinterpret_cast<const f32x4*>(p + 16) : g;
+      float v[4] = {g[0], g[1], g[2], g[3]}, u[4] = {w[0], w[1], w[2], w[3]};
+      finish(a, rows.expert, m, wave_col + c, in, v, u);
+      if (f8_out) {
+        *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
+        float top = largest(v, in, 0.0f);
+        for (int off = lanes / 2; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
+        if (c == 0) tops[wn * S::BM + wm * S::TM + j * 16 + r] = top;
+      } else if (in > 0) {
+        store_four(a.out, m * a.ld_out + wave_col + c, a.out_type, in, v);
       }
     }
-  }
-  if (a.out_type != WB_F8E4M3) return;
-
-  // fp8: the largest magnitude of 128 columns, over the wavefronts that hold them
-  float* tops = reinterpret_cast<float*>(lds + 2 * S::kStage);
-  const int span = kScaleBlock / (a.gated ? S::TN / 2 : S::TN);  // wavefronts
-  __syncthreads();
-#pragma unroll
-  for (int j = 0; j < S::FM; ++j) {
-    top[j] = fmaxf(top[j], __shfl_xor(top[j], 16));
-    top[j] = fmaxf(top[j], __shfl_xor(top[j], 32));
-    if (quad == 0) tops[wn * S::BM + wm * S::TM + j * 16 + l15] = top[j];
-  }
-  __syncthreads();
-#pragma unroll
-  for (int j = 0; j < S::FM; ++j) {
-    const int64_t m = rows.first + wm * S::TM + j * 16 + l15;
-    if (m >= rows.end) continue;
-    float most = 0.0f;
-    for (int w = wn / span * span; w < wn / span * span + span; ++w)
-      most = fmaxf(most, tops[w * S::BM + wm * S::TM + j * 16 + l15]);
-    const RowScale q = row_scale(most);
-    if (quad == 0 && wn % span == 0 && wave_col < a.n_out) a.out_scales[m * a.ld_os + wave_col / kScaleBlock] = q.s;
-#pragma unroll
-    for (int b = 0; b < S::FN; ++b) {
-      if (b >= blocks) break;
-      const int col = wave_col + b * 16, in_row = a.n_out - col;
-      if (in_row <= 0) continue;
-      float v[4];
-      for (int r = 0; r < 4; ++r) v[r] = quotient(acc[b][j][r], q);
-      store_four(a.out, m * a.ld_out + col, WB_F8E4M3, in_row, v);
+    if (f8_out) {
+      // the largest magnitude of 128 columns, over the wavefronts that hold them
+      __syncthreads();
+#pragma unroll 1
+      for (int r = first_r; r < 16; r += per) {
+        const int64_t m = rows.first + wm * S::TM + j * 16 + r;
+        if (m >= rows.end || in_row <= 0) continue;
+        float most = 0.0f;
+        for (int w = wn / span * span; w < wn / span * span + span; ++w)
+          most = fmaxf(most, tops[w * S::BM + wm * S::TM + j * 16 + r]);
+        const RowScale q = row_scale(most);
+        if (c == 0 && wn % span == 0) a.out_scales[m * a.ld_os + wave_col / kScaleBlock] = q.s;
+        const f32x4 g = *reinterpret_cast<const f32x4*>(mine + r * kPitch + at);
+        float v[4];
+        for (int e = 0; e < 4; ++e) v[e] = quotient(g[e], q);
+        store_four(a.out, m * a.ld_out + wave_col + c, WB_F8E4M3, in_row, v);
+      }
     }
   }
 }
 
-// Few rows: the weight is read once, so its bytes are the floor. A wavefront
-// takes CB blocks of sixteen rows of the weight (gated: gate and up of the
-// same columns) against NT * 16 tokens and every KS-th stage of k, straight
-// from memory into operands; the KS partial sums meet in LDS and are added in
-// order. FB such groups make a workgroup: eight where the output is fp8, so
-// that it holds the 128 columns of a scale. The sixteen rows of a block share
-// their weight scales (the launch sees to that).
-template <int NT_, int CB_, int FB_, int KS_, bool GATED_>
-struct Few {
-  static constexpr int NT = NT_, CB = CB_, FB = FB_, KS = KS_, kThreads = 64 * FB * KS;
-  static constexpr bool GATED = GATED_;
-  static constexpr int OB = GATED ? 1 : CB, kCols = 16 * OB * FB, kRows = 16 * NT;
-  static constexpr int kItems = (OB * NT + KS - 1) / KS;      // 16x16 blocks a wavefront finishes
-  // stages whose loads are in flight together, as many as the registers hold
-  static constexpr int kAhead = NT + CB <= (kThreads == 1024 ? 2 : 3) ? 4 : 2;
-  static_assert(!GATED || CB == 2, "gate and up");
-};
-
-template <class S, bool F8>
-__global__ __launch_bounds__(S::kThreads) void wb_linear_few_kernel(LinearArgs a, uint32_t tiles_n) {
-  __shared__ f32x4 sums[S::FB * S::KS][S::CB * S::NT][64];
-  __shared__ float tops[S::FB][S::kRows];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int fb = wave / S::KS, ks = wave % S::KS, l15 = lane & 15, quad = lane >> 4;
-  RowTile rows;
-  if (!find_rows(a, blockIdx.x / tiles_n, S::kRows, rows)) return;
-  const int col0 = static_cast<int>(blockIdx.x % tiles_n) * S::kCols + fb * 16 * S::OB;
-  const int64_t k_bytes = F8 ? int64_t(a.k) : 2 * int64_t(a.k);
-  const int whole = static_cast<int>(k_bytes / kStageBytes), stages = static_cast<int>((k_bytes + kStageBytes - 1) / kStageBytes);
-
-  const uint8_t *w[S::CB], *x[S::NT];
-  const ConstFloat* sw[S::CB];
-  const float* sx[S::NT];
-#pragma unroll
-  for (int c = 0; c < S::CB; ++c) {
-    const int first = S::GATED ? c * a.n_out + min(col0, a.n_out - 1) : min(col0 + 16 * c, a.n - 1);
-    const int last = S::GATED ? (c + 1) * a.n_out - 1 : a.n - 1;
-    w[c] = a.weight + rows.expert * a.stride_w_bytes + int64_t(min(first + l15, last)) * a.ld_w_bytes + quad * 16;
-    if constexpr (F8)
-      sw[c] = (const ConstFloat*)(a.weight_scales + rows.expert * a.stride_ws + int64_t(first / kScaleBlock) * a.ld_ws);
-  }
-#pragma unroll
-  for (int j = 0; j < S::NT; ++j) {
-    const int64_t r = x_row(a, min(rows.first + j * 16 + l15, rows.end - 1));
-    x[j] = a.x + r * a.ld_x_bytes + quad * 16;
-    if constexpr (F8) sx[j] = a.x_scales + r * a.ld_xs;
-  }
-
-  f32x4 acc[S::CB][S::NT];
-#pragma unroll
-  for (int c = 0; c < S::CB; ++c)
-#pragma unroll
-    for (int j = 0; j < S::NT; ++j) acc[c][j] = f32x4{0, 0, 0, 0};
-
-  struct Stage {
-    u32x4 w[S::CB][2], x[S::NT][2];
-    float sw[S::CB], sx[S::NT];
-  };
-  auto load = [&](Stage& t, int s) {
-    const int64_t at = int64_t(s) * kStageBytes;
-#pragma unroll
-    for (int c = 0; c < S::CB; ++c) {
-      t.w[c][0] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_a1*>(w[c] + at));
-      t.w[c][1] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_a1*>(w[c] + at + 64));
-      if constexpr (F8) t.sw[c] = sw[c][s];
-    }
-#pragma unroll
-    for (int j = 0; j < S::NT; ++j) {
-      t.x[j][0] = *reinterpret_cast<const u32x4_a1*>(x[j] + at);
-      t.x[j][1] = *reinterpret_cast<const u32x4_a1*>(x[j] + at + 64);
-      if constexpr (F8) t.sx[j] = sx[j][s];
-    }
-  };
-  auto add = [&](const Stage& t) {
-    Operand<F8> xo[S::NT];
-#pragma unroll
-    for (int j = 0; j < S::NT; ++j) xo[j] = Operand<F8>(__builtin_bit_cast(i32x4, t.x[j][0]), __builtin_bit_cast(i32x4, t.x[j][1]));
-#pragma unroll
-    for (int c = 0; c < S::CB; ++c) {
-      const Operand<F8> wo(__builtin_bit_cast(i32x4, t.w[c][0]), __builtin_bit_cast(i32x4, t.w[c][1]));
-#pragma unroll
-      for (int j = 0; j < S::NT; ++j) {
-        if constexpr (F8) {
-          const f32x4 part = block_sum<F8>(wo, xo[j], f32x4{0, 0, 0, 0});
-          const float both = t.sx[j] * t.sw[c];
-          for (int r = 0; r < 4; ++r) acc[c][j][r] = __builtin_fmaf(part[r], both, acc[c][j][r]);
-        } else {
-          acc[c][j] = block_sum<F8>(wo, xo[j], acc[c][j]);
-        }
-      }
-    }
-  };
-  int s = ks;
-  for (; s + (S::kAhead - 1) * S::KS < whole; s += S::kAhead * S::KS) {
-    Stage t[S::kAhead];
-#pragma unroll
-    for (int u = 0; u < S::kAhead; ++u) load(t[u], s + u * S::KS);
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int u = 0; u < S::kAhead; ++u) add(t[u]);
-  }
-  for (; s < stages; s += S::KS) {
-    Stage t;
-    if (s < whole) {
-      load(t, s);
-    } else {  // the end of k
-      const int64_t at = int64_t(s) * kStageBytes + quad * 16;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-#pragma unroll
-        for (int c = 0; c < S::CB; ++c) t.w[c][h] = load_piece(w[c] - quad * 16, at + 64 * h, k_bytes);
-#pragma unroll
-        for (int j = 0; j < S::NT; ++j) t.x[j][h] = load_piece(x[j] - quad * 16, at + 64 * h, k_bytes);
-      }
-      if constexpr (F8) {
-#pragma unroll
-        for (int c = 0; c < S::CB; ++c) t.sw[c] = sw[c][s];
-#pragma unroll
-        for (int j = 0; j < S::NT; ++j) t.sx[j] = sx[j][s];
-      }
-    }
-    add(t);
-  }
-
-#pragma unroll
-  for (int c = 0; c < S::CB; ++c)
-#pragma unroll
-    for (int j = 0; j < S::NT; ++j) sums[wave][c * S::NT + j][lane] = acc[c][j];
-  __syncthreads();
-  auto total = [&](int c, int j, float(&v)[4]) {
-    f32x4 t = sums[fb * S::KS][c * S::NT + j][lane];
-    for (int i = 1; i < S::KS; ++i) {
-      const f32x4 p = sums[fb * S::KS + i][c * S::NT + j][lane];
-      for (int r = 0; r < 4; ++r) t[r] += p[r];
-    }
-    for (int r = 0; r < 4; ++r) v[r] = t[r];
-  };
-  float v[S::kItems][4];
-#pragma unroll
-  for (int i = 0; i < S::kItems; ++i) {
-    const int item = ks + i * S::KS;
-    if (item >= S::OB * S::NT) break;
-    const int c = item / S::NT, j = item % S::NT, col = col0 + c * 16 + quad * 4;
-    const int64_t m = rows.first + j * 16 + l15;
-    const int in_row = m < rows.end ? a.n_out - col : 0;
-    float u[4] = {1.0f, 1.0f, 1.0f, 1.0f};
-    total(c, j, v[i]);
-    if constexpr (S::GATED) total(1, j, u);
-    finish(a, rows.expert, m, col, in_row, v[i], u);
-    if (a.out_type != WB_F8E4M3) {
-      if (in_row > 0) store_four(a.out, m * a.ld_out + col, a.out_type, in_row, v[i]);
-      continue;
-    }
-    float top = largest(v[i], in_row, 0.0f);
-    top = fmaxf(top, __shfl_xor(top, 16));
-    top = fmaxf(top, __shfl_xor(top, 32));
-    if (quad == 0) tops[fb][j * 16 + l15] = top;
-  }
-  if (a.out_type != WB_F8E4M3) return;
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < S::kItems; ++i) {
-    const int item = ks + i * S::KS;
-    if (item >= S::OB * S::NT) break;
-    const int j = item % S::NT, col = col0 + quad * 4;
-    const int64_t m = rows.first + j * 16 + l15;
-    const int in_row = m < rows.end ? a.n_out - col : 0;
-    if (in_row <= 0) continue;
-    float most = 0.0f;
-    for (int f = 0; f < S::FB; ++f) most = fmaxf(most, tops[f][j * 16 + l15]);
-    const RowScale q = row_scale(most);
-    if (quad == 0 && fb == 0) a.out_scales[m * a.ld_os + col / kScaleBlock] = q.s;
-    for (int r = 0; r < 4; ++r) v[i][r] = quotient(v[i][r], q);
-    store_four(a.out, m * a.ld_out + col, WB_F8E4M3, in_row, v[i]);
+// fp8 codes and scales of fp32 rows, for tiles too narrow to hold the 128
+// columns of a scale: sixteen lanes a scale, eight columns each. Rows that
+// belong to no expert are left alone.
+__global__ __launch_bounds__(256) void wb_linear_codes_kernel(const float* sums, LinearArgs a) {
+  const int64_t row = blockIdx.x, c = (int64_t(blockIdx.y) * 256 + threadIdx.x) * 8;
+  if (a.offsets && (row < a.offsets[0] || row >= a.offsets[a.num_experts])) return;
+  if (c - (threadIdx.x & 15) * 8 >= a.n_out) return;
+  const float* from = sums + row * a.n_out;
+  float v[8];
+  if (c + 8 <= a.n_out)
+    load_eight(from, c, WB_F32, v);
+  else
+    load_tail(from, c, a.n_out, WB_F32, v);
+  float top = 0.0f;
+  for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(v[i]));
+  const RowScale q = row_scale(reduce16(top, FMax()));
+  if ((threadIdx.x & 15) == 0) a.out_scales[row * a.ld_os + c / kScaleBlock] = q.s;
+  for (int i = 0; i < 8; ++i) v[i] = quotient(v[i], q);
+  uint8_t* to = static_cast<uint8_t*>(a.out) + row * a.ld_out + c;
+  const u32x2 p = {pack_fp8(v[0], v[1], v[2], v[3]), pack_fp8(v[4], v[5], v[6], v[7])};
+  if (c + 8 <= a.n_out) {
+    *reinterpret_cast<u32x2_a1*>(to) = p;
+  } else {
+    for (int i = 0; i < 8; ++i)
+      if (c + i < a.n_out) to[i] = static_cast<uint8_t>(p[i >> 2] >> (8 * (i & 3)));
   }
 }
 
@@ -636,27 +537,6 @@ __global__ __launch_bounds__(S::kThreads) void wb_linear_few_kernel(LinearArgs a
 int64_t row_tiles(const LinearArgs& a, int per) {
   if (!a.offsets) return (a.rows + per - 1) / per;
   return std::min<int64_t>(a.rows, a.rows / per + std::min<int64_t>(a.num_experts, a.rows));
-}
-
-template <class S>
-hipError_t launch_few(const LinearArgs& a, hipStream_t st) {
-  const int64_t tiles_n = (a.n_out + S::kCols - 1) / S::kCols, all = row_tiles(a, S::kRows) * tiles_n;
-  if (all > 0x3fffff) return hipErrorInvalidConfiguration;
-  const dim3 grid(static_cast<uint32_t>(all)), block(S::kThreads);
-  if (a.in_type == WB_F8E4M3)
-    hipLaunchKernelGGL((wb_linear_few_kernel<S, true>), grid, block, 0, st, a, static_cast<uint32_t>(tiles_n));
-  else
-    hipLaunchKernelGGL((wb_linear_few_kernel<S, false>), grid, block, 0, st, a, static_cast<uint32_t>(tiles_n));
-  return hipGetLastError();
-}
-
-// NT * 16 tokens at a time.
-template <int NT>
-hipError_t launch_few_rows(const LinearArgs& a, hipStream_t st) {
-  constexpr int kSplit = NT == 1 ? 2 : 1;  // of k, in the workgroups of eight groups
-  if (a.out_type == WB_F8E4M3)
-    return a.gated ? launch_few<Few<NT, 2, 8, kSplit, true>>(a, st) : launch_few<Few<NT, 1, 8, kSplit, false>>(a, st);
-  return a.gated ? launch_few<Few<NT, 2, 1, 8, true>>(a, st) : launch_few<Few<NT, 1, 1, 8, false>>(a, st);
 }
 
 template <class S, bool F8, bool DIRECT>
@@ -673,24 +553,94 @@ hipError_t launch_tile(const LinearArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
-template <class S>
+
+
+// The tiles in use. A launch takes the one whose rounds over the 256 CUs are
+// expected to be done first: rounds * us, the measured time of a round per
+// stage of k with every CU busy, for bf16 and for fp8 (twice the k in a
+// stage), `resident` workgroups share a
+// CU, which pays from 256 tiles on: us_few holds for fewer. Large tiles read
+// less per product; small ones give every CU work, and more of them: for 333 x
+// 3456 x 1536 in bf16 64 x 64 takes 13 us and 256 x 256 50, for 8192 x 8192 x
+// 8192 1.66 ms and 0.89.
+struct Choice {
+  int bm, bn, resident;
+  bool direct_only;
+  float us[2], us_few[2];  // bf16, fp8
+};
+constexpr Choice kChoices[] = {
+    {16, 32, 1, true, {0.14f, 0.17f}, {0.14f, 0.17f}},   {32, 32, 1, false, {0.18f, 0.21f}, {0.18f, 0.21f}},
+    {32, 64, 1, true, {0.25f, 0.32f}, {0.25f, 0.32f}},   {64, 64, 2, false, {0.56f, 0.74f}, {0.50f, 0.52f}},
+    {64, 64, 1, true, {0.33f, 0.49f}, {0.33f, 0.49f}},   {128, 64, 1, true, {0.46f, 0.83f}, {0.46f, 0.83f}},
+    {128, 128, 2, false, {1.18f, 2.25f}, {1.00f, 1.50f}}, {128, 128, 1, true, {0.86f, 1.25f}, {0.86f, 1.25f}},
+    {256, 256, 1, true, {1.72f, 3.90f}, {1.72f, 3.90f}},
+};
+constexpr int kNumChoices = sizeof(kChoices) / sizeof(kChoices[0]);
+
+int choose(const LinearArgs& a) {
+  const int f8 = a.in_type == WB_F8E4M3;
+  int best = -1;
+  double least = 0.0;
+  for (int i = 0; i < kNumChoices; ++i) {
+    const Choice& c = kChoices[i];
+    if (c.direct_only && !a.direct) continue;
+    const int step = a.gated ? c.bn / 2 : c.bn;
+    // of the experts' last tiles about half are empty
+    double tiles_m = double(row_tiles(a, c.bm));
+    if (a.offsets) tiles_m = std::min(double(a.rows), double(a.rows) / c.bm + 0.5 * std::min<int64_t>(a.num_experts, a.rows));
+    const double tiles = tiles_m * ((a.n_out + step - 1) / step);
+    const double us = tiles <= 256 ? c.us_few[f8] : std::ceil(tiles / (256.0 * c.resident)) * c.us[f8];
+    if (best < 0 || us < least) best = i, least = us;
+  }
+  return best;
+}
+
+// Whether a tile holds whole scales of an fp8 output.
+bool holds_scales(const LinearArgs& a, int choice) {
+  return (a.gated ? kChoices[choice].bn / 2 : kChoices[choice].bn) % kScaleBlock == 0;
+}
+
+template <class S, bool ANY>
 hipError_t launch_shape(const LinearArgs& a, hipStream_t st) {
-  if (a.in_type == WB_F8E4M3) return a.direct ? launch_tile<S, true, true>(a, st) : launch_tile<S, true, false>(a, st);
-  return a.direct ? launch_tile<S, false, true>(a, st) : launch_tile<S, false, false>(a, st);
+  if constexpr (ANY) {
+    if (!a.direct) return a.in_type == WB_F8E4M3 ? launch_tile<S, true, false>(a, st) : launch_tile<S, false, false>(a, st);
+  }
+  return a.in_type == WB_F8E4M3 ? launch_tile<S, true, true>(a, st) : launch_tile<S, false, true>(a, st);
+}
+
+hipError_t launch_choice(const LinearArgs& a, int choice, hipStream_t st) {
+  switch (choice) {
+    case 0: return launch_shape<Shape<16, 32, 1, 1, 4, 4, 4>, false>(a, st);
+    case 1: return launch_shape<Shape<32, 32, 2, 1, 4, 4, 4>, true>(a, st);
+    case 2: return launch_shape<Shape<32, 64, 2, 2, 2, 4, 3>, false>(a, st);
+    case 3: return launch_shape<Shape<64, 64, 2, 2, 2, 2, 2>, true>(a, st);
+    case 4: return launch_shape<Shape<64, 64, 2, 2, 2, 2, 4>, false>(a, st);
+    case 5: return launch_shape<Shape<128, 64, 4, 2, 1, 2, 3>, false>(a, st);
+    case 6: return launch_shape<Shape<128, 128, 2, 2, 1, 1, 2>, true>(a, st);
+    case 7: return launch_shape<Shape<128, 128, 2, 2, 2, 2, 2>, false>(a, st);
+    default: return launch_shape<Shape<256, 256, 4, 2, 1, 1, 2>, false>(a, st);
+  }
 }
 
 }  // namespace
 
-int launch_linear(const LinearArgs& a, void* stream) {
+size_t linear_workspace_bytes(const LinearArgs& a) {
+  if (a.rows == 0 || a.out_type != WB_F8E4M3 || holds_scales(a, choose(a))) return 0;
+  return static_cast<size_t>(a.rows) * a.n_out * sizeof(float);
+}
+
+int launch_linear(const LinearArgs& a, void* workspace, void* stream) {
   if (a.rows == 0) return hipSuccess;
   const auto st = static_cast<hipStream_t>(stream);
-  const int64_t each = a.offsets ? a.rows / a.num_experts : a.rows;  // rows a weight meets
-  const bool shared_scales = a.in_type != WB_F8E4M3 || !a.gated || a.n_out % 16 == 0;
-  if (!shared_scales) return launch_shape<Shape<64, 256, 1, 4>>(a, st);
-  if (each <= 16) return launch_few_rows<1>(a, st);
-  if (each <= 32) return launch_few_rows<2>(a, st);
-  if (each <= 64) return launch_few_rows<4>(a, st);
-  return launch_shape<Shape<64, 256, 1, 4>>(a, st);
+  const int choice = choose(a);
+  if (a.out_type != WB_F8E4M3 || holds_scales(a, choice)) return launch_choice(a, choice, st);
+  LinearArgs sums = a;
+  sums.out = workspace, sums.out_type = WB_F32, sums.ld_out = a.n_out;
+  const hipError_t e = launch_choice(sums, choice, st);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(wb_linear_codes_kernel, dim3(static_cast<uint32_t>(a.rows), static_cast<uint32_t>((a.n_out + 2047) / 2048)),
+                     dim3(256), 0, st, static_cast<const float*>(workspace), a);
+  return hipGetLastError();
 }
 
 }  // namespace wb

@@ -94,13 +94,14 @@ struct LinearArgs {
 };
 
 size_t route_workspace_bytes(int64_t rows, int32_t experts);
+size_t linear_workspace_bytes(const LinearArgs& a);
 
 // Each enqueues its kernels on the stream and returns a hipError_t.
 int launch_add_rms_norm(const NormArgs& a, void* stream);
 int launch_route(const RouteArgs& a, void* stream);
 int launch_route_grad(const RouteGradArgs& a, void* stream);
 int launch_combine(const CombineArgs& a, void* stream);
-int launch_linear(const LinearArgs& a, void* stream);
+int launch_linear(const LinearArgs& a, void* workspace, void* stream);
 
 }  // namespace wb
 

@@ -106,6 +106,72 @@ int check_route(const wb_matrix* logits, const uint8_t* mask, int32_t k, Operand
   return ops.rc;
 }
 
+// The checks of wb_linear and, after them, its launch's arguments.
+int check_linear(const wb_linear_args* p, Operands& ops, wb::LinearArgs& a) {
+  if (!p) return set_error(WB_EINVAL, "null argument");
+  const bool stacked = p->num_experts > 0;
+  if (p->num_experts < 0 || p->num_experts > 65536) return set_error(WB_EINVAL, "num_experts outside 0..65536");
+  int rc = too_many_rows(p->x.rows);
+  if (rc == WB_OK) rc = too_many_rows(p->out.rows);
+  if (rc != WB_OK) return rc;
+  if (p->x.dtype != p->weight.dtype || (p->x.dtype != WB_BF16 && p->x.dtype != WB_F8E4M3))
+    return set_error(WB_EUNSUPPORTED, "x and weight must both be bf16 or both fp8");
+  if (p->activation < WB_ACT_NONE || p->activation > WB_ACT_GELU) return set_error(WB_EINVAL, "unknown activation");
+  if (!stacked && (p->offsets || p->tokens)) return set_error(WB_EINVAL, "offsets and tokens need num_experts");
+  if (stacked && !p->offsets) return set_error(WB_EINVAL, "stacked weights need offsets");
+  const int64_t e = stacked ? p->num_experts : 1, k = p->x.cols;
+  if (p->weight.rows < 1 || p->weight.rows % e != 0) return set_error(WB_EINVAL, "weight rows are no multiple of num_experts");
+  const int64_t n = p->weight.rows / e;
+  if (n > kMaxCols) return set_error(WB_EUNSUPPORTED, "weight of more than 2^28 rows");
+  if (p->gated && n % 2 != 0) return set_error(WB_EINVAL, "gated weight with an odd number of rows");
+  const int64_t n_out = p->gated ? n / 2 : n, rows = stacked ? p->out.rows : p->x.rows;
+  if (stacked && !p->tokens && p->x.rows != rows)
+    return set_error(WB_EINVAL, "without tokens, x has as many rows as out");
+  if (stacked && p->tokens && p->x.rows == 0 && rows > 0) return set_error(WB_EINVAL, "tokens of an x without rows");
+  const bool f8 = p->x.dtype == WB_F8E4M3;
+  ops.matrix(p->x, p->x.rows, k, "x");
+  ops.matrix(p->weight, p->weight.rows, k, "weight");
+  if (f8) {
+    ops.scales(p->x_scales, p->x.rows, ceil_div(k, wb::kScaleBlock), "x_scales");
+    ops.scales(p->weight_scales, e * ceil_div(n, wb::kScaleBlock), ceil_div(k, wb::kScaleBlock), "weight_scales");
+  } else if (p->x_scales.data || p->weight_scales.data) {
+    return set_error(WB_EINVAL, "scales are given for operands that are not fp8");
+  }
+  if (p->bias.data) {
+    ops.floats(p->bias, "bias");
+    ops.matrix(p->bias, e, n, "bias");
+  }
+  if (p->residual.data) {
+    ops.floats(p->residual, "residual");
+    ops.matrix(p->residual, rows, n_out, "residual");
+  }
+  ops.result(p->out, &p->out_scales, rows, n_out);
+  if (stacked) ops.array(p->offsets, e + 1, 4, "offsets");
+  if (p->tokens) ops.array(p->tokens, rows, 4, "tokens");
+  if (ops.rc != WB_OK) return ops.rc;
+
+  const int64_t es = f8 ? 1 : 2;
+  a.x = static_cast<const uint8_t*>(p->x.data), a.weight = static_cast<const uint8_t*>(p->weight.data);
+  a.ld_x_bytes = p->x.ld * es, a.ld_w_bytes = p->weight.ld * es, a.stride_w_bytes = n * a.ld_w_bytes;
+  a.rows = rows, a.x_rows = p->x.rows, a.n = static_cast<int32_t>(n), a.n_out = static_cast<int32_t>(n_out);
+  a.k = static_cast<int32_t>(k), a.in_type = p->x.dtype, a.gated = p->gated != 0, a.activation = p->activation;
+  a.num_experts = p->num_experts, a.offsets = p->offsets, a.tokens = p->tokens;
+  if (f8) {
+    a.x_scales = static_cast<const float*>(p->x_scales.data), a.ld_xs = p->x_scales.ld;
+    a.weight_scales = static_cast<const float*>(p->weight_scales.data), a.ld_ws = p->weight_scales.ld;
+    a.stride_ws = ceil_div(n, wb::kScaleBlock) * a.ld_ws;
+  }
+  if (p->bias.data) a.bias = p->bias.data, a.bias_type = p->bias.dtype, a.stride_bias = p->bias.ld;
+  if (p->residual.data) a.residual = p->residual.data, a.residual_type = p->residual.dtype, a.ld_residual = p->residual.ld;
+  a.out = p->out.data, a.out_type = p->out.dtype, a.ld_out = p->out.ld;
+  if (p->out.dtype == WB_F8E4M3) a.out_scales = static_cast<float*>(p->out_scales.data), a.ld_os = p->out_scales.ld;
+  const uintptr_t at = reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.weight) |
+                       static_cast<uintptr_t>(a.ld_x_bytes) | static_cast<uintptr_t>(a.ld_w_bytes) |
+                       static_cast<uintptr_t>(k * es);
+  a.direct = at % 16 == 0 && !(f8 && a.gated && n_out % 16 != 0);
+  return WB_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -213,72 +279,30 @@ int wb_route_backward(const wb_matrix* logits, const uint8_t* mask, int32_t k, i
   });
 }
 
-int wb_linear(const wb_linear_args* p, void* stream) {
+int wb_linear_workspace(const wb_linear_args* p, size_t* bytes) {
   return guarded([&]() -> int {
-    if (!p) return set_error(WB_EINVAL, "null argument");
-    const bool stacked = p->num_experts > 0;
-    if (p->num_experts < 0 || p->num_experts > 65536) return set_error(WB_EINVAL, "num_experts outside 0..65536");
-    int rc = too_many_rows(p->x.rows);
-    if (rc == WB_OK) rc = too_many_rows(p->out.rows);
-    if (rc != WB_OK) return rc;
-    if (p->x.dtype != p->weight.dtype || (p->x.dtype != WB_BF16 && p->x.dtype != WB_F8E4M3))
-      return set_error(WB_EUNSUPPORTED, "x and weight must both be bf16 or both fp8");
-    if (p->activation < WB_ACT_NONE || p->activation > WB_ACT_GELU) return set_error(WB_EINVAL, "unknown activation");
-    if (!stacked && (p->offsets || p->tokens)) return set_error(WB_EINVAL, "offsets and tokens need num_experts");
-    if (stacked && !p->offsets) return set_error(WB_EINVAL, "stacked weights need offsets");
-    const int64_t e = stacked ? p->num_experts : 1, k = p->x.cols;
-    if (p->weight.rows < 1 || p->weight.rows % e != 0) return set_error(WB_EINVAL, "weight rows are no multiple of num_experts");
-    const int64_t n = p->weight.rows / e;
-    if (n > kMaxCols) return set_error(WB_EUNSUPPORTED, "weight of more than 2^28 rows");
-    if (p->gated && n % 2 != 0) return set_error(WB_EINVAL, "gated weight with an odd number of rows");
-    const int64_t n_out = p->gated ? n / 2 : n, rows = stacked ? p->out.rows : p->x.rows;
-    if (stacked && !p->tokens && p->x.rows != rows)
-      return set_error(WB_EINVAL, "without tokens, x has as many rows as out");
-    if (stacked && p->tokens && p->x.rows == 0 && rows > 0) return set_error(WB_EINVAL, "tokens of an x without rows");
-    const bool f8 = p->x.dtype == WB_F8E4M3;
+    if (!bytes) return set_error(WB_EINVAL, "null argument");
     Operands ops;
-    ops.matrix(p->x, p->x.rows, k, "x");
-    ops.matrix(p->weight, p->weight.rows, k, "weight");
-    if (f8) {
-      ops.scales(p->x_scales, p->x.rows, ceil_div(k, wb::kScaleBlock), "x_scales");
-      ops.scales(p->weight_scales, e * ceil_div(n, wb::kScaleBlock), ceil_div(k, wb::kScaleBlock), "weight_scales");
-    } else if (p->x_scales.data || p->weight_scales.data) {
-      return set_error(WB_EINVAL, "scales are given for operands that are not fp8");
-    }
-    if (p->bias.data) {
-      ops.floats(p->bias, "bias");
-      ops.matrix(p->bias, e, n, "bias");
-    }
-    if (p->residual.data) {
-      ops.floats(p->residual, "residual");
-      ops.matrix(p->residual, rows, n_out, "residual");
-    }
-    ops.result(p->out, &p->out_scales, rows, n_out);
-    if (stacked) ops.array(p->offsets, e + 1, 4, "offsets");
-    if (p->tokens) ops.array(p->tokens, rows, 4, "tokens");
-    if (ops.rc != WB_OK) return ops.rc;
-
     wb::LinearArgs a{};
-    const int64_t es = f8 ? 1 : 2;
-    a.x = static_cast<const uint8_t*>(p->x.data), a.weight = static_cast<const uint8_t*>(p->weight.data);
-    a.ld_x_bytes = p->x.ld * es, a.ld_w_bytes = p->weight.ld * es, a.stride_w_bytes = n * a.ld_w_bytes;
-    a.rows = rows, a.x_rows = p->x.rows, a.n = static_cast<int32_t>(n), a.n_out = static_cast<int32_t>(n_out);
-    a.k = static_cast<int32_t>(k), a.in_type = p->x.dtype, a.gated = p->gated != 0, a.activation = p->activation;
-    a.num_experts = p->num_experts, a.offsets = p->offsets, a.tokens = p->tokens;
-    if (f8) {
-      a.x_scales = static_cast<const float*>(p->x_scales.data), a.ld_xs = p->x_scales.ld;
-      a.weight_scales = static_cast<const float*>(p->weight_scales.data), a.ld_ws = p->weight_scales.ld;
-      a.stride_ws = ceil_div(n, wb::kScaleBlock) * a.ld_ws;
-    }
-    if (p->bias.data) a.bias = p->bias.data, a.bias_type = p->bias.dtype, a.stride_bias = p->bias.ld;
-    if (p->residual.data) a.residual = p->residual.data, a.residual_type = p->residual.dtype, a.ld_residual = p->residual.ld;
-    a.out = p->out.data, a.out_type = p->out.dtype, a.ld_out = p->out.ld;
-    if (p->out.dtype == WB_F8E4M3) a.out_scales = static_cast<float*>(p->out_scales.data), a.ld_os = p->out_scales.ld;
-    const uintptr_t at = reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.weight) |
-                         static_cast<uintptr_t>(a.ld_x_bytes) | static_cast<uintptr_t>(a.ld_w_bytes) |
-                         static_cast<uintptr_t>(k * es);
-    a.direct = at % 16 == 0 && !(f8 && a.gated && n_out % 16 != 0);
-    const int launch = wb::launch_linear(a, stream);
+    const int rc = check_linear(p, ops, a);
+    if (rc != WB_OK) return rc;
+    *bytes = wb::linear_workspace_bytes(a);
+    return WB_OK;
+  });
+}
+
+int wb_linear(const wb_linear_args* p, void* workspace, size_t workspace_bytes, void* stream) {
+  return guarded([&]() -> int {
+    Operands ops;
+    wb::LinearArgs a{};
+    const int rc = check_linear(p, ops, a);
+    if (rc != WB_OK) return rc;
+    const size_t need = wb::linear_workspace_bytes(a);
+    if (workspace_bytes < need) return set_error(WB_ESIZE, "workspace smaller than wb_linear_workspace");
+    if (need)
+      ops.rc = check_extent_as(workspace, static_cast<int64_t>(need), [] { return std::string("workspace"); }, 16, &ops.range);
+    if (ops.rc != WB_OK) return ops.rc;
+    const int launch = wb::launch_linear(a, workspace, stream);
     if (launch == hipErrorInvalidConfiguration) return set_error(WB_EUNSUPPORTED, "more tiles than one launch takes");
     return launched(launch, "product launch");
   });

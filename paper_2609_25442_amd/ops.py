@@ -201,7 +201,7 @@ def expert_linear(x, weight, offsets, tokens=None, bias=None, *, x_scales=None, 
 
 
 def _linear(x, weight, offsets, tokens, x_scales, weight_scales, bias, residual, activation, gated, out_dtype):
-    r = _args.linear(_address("wb_linear"), x, weight, offsets, tokens, x_scales, weight_scales, bias, residual,
+    r = _args.linear(_address("wb_linear"), _address("wb_linear_workspace"), x, weight, offsets, tokens, x_scales, weight_scales, bias, residual,
                      _type(activation, ACTIVATIONS, "activation"), bool(gated), _type(out_dtype, DTYPES, "out_dtype"),
                      *_here())
     return _refused(r) if isinstance(r, (str, int)) else r

@@ -3,6 +3,7 @@ strides, types and masks where a kernel can go wrong. Tolerances follow from
 the operations (ops_ref): fp32 sums of so many terms, one rounding to the
 output's type."""
 
+import ctypes
 import math
 
 import pytest
@@ -388,7 +389,7 @@ def test_expert_linear_leaves_other_ranks_rows():
         out = torch.full((50, n), 7.0, dtype=torch.bfloat16, device="cuda")
         got = out.clone()
         args = ref_args(x, w, got, torch.tensor([lo, a, b, hi], dtype=torch.int32, device="cuda"))
-        assert lib.wb_linear(*args[:1], None) == 0, lib.wb_last_error()
+        assert lib.wb_linear(args[0], None, ctypes.c_size_t(0), None) == 0, lib.wb_last_error()
         torch.cuda.synchronize()
         first, last = max(lo, 0), min(hi, 50)
         assert torch.all(got[:first] == 7) and torch.all(got[last:] == 7)
@@ -398,8 +399,6 @@ def test_expert_linear_leaves_other_ranks_rows():
 
 
 def ref_args(x, w, out, offsets):
-    import ctypes
-
     class Matrix(ctypes.Structure):
         _fields_ = [("data", ctypes.c_void_p), ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32),
                     ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("ld", ctypes.c_int64)]
