@@ -154,11 +154,10 @@ __device__ __forceinline__ void store_four(void* base, int64_t at, int type, int
   }
 }
 
-// What follows the sums of a row m and four columns from col on; u are the
-// sums of the up rows where the weight is gated. in_row: columns that exist
-// (none for a row past the end).
-__device__ __forceinline__ void finish(const LinearArgs& a, int expert, int64_t m, int col, int in_row, float (&v)[4],
-                                       float (&u)[4]) {
+// What becomes of the sums of four columns from col on; u are the sums of the
+// up rows where the weight is gated. in_row: columns that exist (none for a
+// row past the end).
+__device__ __forceinline__ void finish(const LinearArgs& a, int expert, int col, int in_row, float (&v)[4], float (&u)[4]) {
   if (a.bias && in_row > 0) {
     for (int r = 0; r < 4; ++r) {
       const int c = min(col + r, a.n_out - 1);
@@ -167,11 +166,6 @@ __device__ __forceinline__ void finish(const LinearArgs& a, int expert, int64_t 
     }
   }
   for (int r = 0; r < 4; ++r) v[r] = a.gated ? activate(v[r], a.activation) * u[r] : activate(v[r], a.activation);
-  if (a.residual && in_row > 0) {
-    float add[4];
-    load_four(a.residual, m * a.ld_residual + col, a.residual_type, in_row, add);
-    for (int r = 0; r < 4; ++r) v[r] += add[r];
-  }
 }
 
 __device__ __forceinline__ float largest(const float (&v)[4], int in_row, float top) {
@@ -209,11 +203,14 @@ struct Operand {
   }
 };
 
-template <bool F8>
-__device__ __forceinline__ f32x4 block_sum(const Operand<F8>& w, const Operand<F8>& x, f32x4 c) {
+// The same rows of the weight against M blocks of tokens: the sums of one
+// block depend on each other, those of different blocks do not.
+template <bool F8, int M>
+__device__ __forceinline__ void block_sums(const Operand<F8>& w, const Operand<F8> (&x)[M], f32x4 (&c)[M]) {
 #pragma unroll
-  for (int h = 0; h < (F8 ? 4 : 2); ++h) c = mfma(w.v[h], x.v[h], c);
-  return c;
+  for (int h = 0; h < (F8 ? 4 : 2); ++h)
+#pragma unroll
+    for (int j = 0; j < M; ++j) c[j] = mfma(w.v[h], x[j].v[h], c[j]);
 }
 
 // A workgroup's tile: BM rows of the output by BN rows of the weight, WM x WN
@@ -402,19 +399,21 @@ __global__ __launch_bounds__(S::kThreads) void wb_linear_tile_kernel(LinearArgs 
       if constexpr (F8) {
         const float* sw = sc + S::BM + wn * S::TN + i * 16;
         const f32x4 sr = DIRECT ? f32x4{sw[0], sw[0], sw[0], sw[0]} : *reinterpret_cast<const f32x4*>(sw + quad * 4);
+        f32x4 part[S::FM];
+#pragma unroll
+        for (int j = 0; j < S::FM; ++j) part[j] = f32x4{0, 0, 0, 0};
+        block_sums<F8>(w, x, part);
 #pragma unroll
         for (int j = 0; j < S::FM; ++j) {
-          const f32x4 part = block_sum<F8>(w, x[j], f32x4{0, 0, 0, 0});
           if constexpr (DIRECT) {
             const float both = sx[j] * sr[0];
-            for (int r = 0; r < 4; ++r) acc[i][j][r] = __builtin_fmaf(part[r], both, acc[i][j][r]);
+            for (int r = 0; r < 4; ++r) acc[i][j][r] = __builtin_fmaf(part[j][r], both, acc[i][j][r]);
           } else {
-            for (int r = 0; r < 4; ++r) acc[i][j][r] = __builtin_fmaf(part[r], sx[j] * sr[r], acc[i][j][r]);
+            for (int r = 0; r < 4; ++r) acc[i][j][r] = __builtin_fmaf(part[j][r], sx[j] * sr[r], acc[i][j][r]);
           }
         }
       } else {
-#pragma unroll
-        for (int j = 0; j < S::FM; ++j) acc[i][j] = block_sum<F8>(w, x[j], acc[i][j]);
+        block_sums<F8>(w, x, acc[i]);
       }
     }
     }
@@ -465,24 +464,42 @@ __global__ __launch_bounds__(S::kThreads) void wb_linear_tile_kernel(LinearArgs 
 #pragma unroll
       for (int i = 0; i < S::FN; ++i) *reinterpret_cast<f32x4*>(mine + l15 * kPitch + i * 16 + quad * 4) = acc[i][j];
     }
+    order_lanes();
+    // four of the lane's rows at a time, so that their residuals' loads overlap
 #pragma unroll 1
-    for (int r = first_r; r < 16; r += per) {
-      const int64_t m = rows.first + wm * S::TM + j * 16 + r;
-      const int in = m < rows.end ? in_row : 0;
-      float* p = mine + r * kPitch + at;
-      const f32x4 g = *reinterpret_cast<const f32x4*>(p);
-      const f32x4 w = a.gated ? *reinterpret_cast<const f32x4*>(p + 16) : g;
-      float v[4] = {g[0], g[1], g[2], g[3]}, u[4] = {w[0], w[1], w[2], w[3]};
-      finish(a, rows.expert, m, wave_col + c, in, v, u);
-      if (f8_out) {
-        *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
-        float top = largest(v, in, 0.0f);
-        for (int off = lanes / 2; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
-        if (c == 0) tops[wn * S::BM + wm * S::TM + j * 16 + r] = top;
-      } else if (in > 0) {
-        store_four(a.out, m * a.ld_out + wave_col + c, a.out_type, in, v);
+    for (int r0 = first_r; r0 < 16; r0 += 4 * per) {
+      float add[4][4];
+#pragma unroll
+      for (int h = 0; h < 4; ++h) {
+        const int64_t m = rows.first + wm * S::TM + j * 16 + r0 + h * per;
+        if (a.residual && r0 + h * per < 16 && m < rows.end && in_row > 0)
+          load_four(a.residual, m * a.ld_residual + wave_col + c, a.residual_type, in_row, add[h]);
+        else
+          for (int e = 0; e < 4; ++e) add[h][e] = 0.0f;
+      }
+#pragma unroll
+      for (int h = 0; h < 4; ++h) {
+        const int r = r0 + h * per;
+        if (r >= 16) break;
+        const int64_t m = rows.first + wm * S::TM + j * 16 + r;
+        const int in = m < rows.end ? in_row : 0;
+        float* p = mine + r * kPitch + at;
+        const f32x4 g = *reinterpret_cast<const f32x4*>(p);
+        const f32x4 w = a.gated ? *reinterpret_cast<const f32x4*>(p + 16) : g;
+        float v[4] = {g[0], g[1], g[2], g[3]}, u[4] = {w[0], w[1], w[2], w[3]};
+        finish(a, rows.expert, wave_col + c, in, v, u);
+        for (int e = 0; e < 4; ++e) v[e] += add[h][e];
+        if (f8_out) {
+          *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
+          float top = largest(v, in, 0.0f);
+          for (int off = lanes / 2; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
+          if (c == 0) tops[wn * S::BM + wm * S::TM + j * 16 + r] = top;
+        } else if (in > 0) {
+          store_four(a.out, m * a.ld_out + wave_col + c, a.out_type, in, v);
+        }
       }
     }
+    order_lanes();
     if (f8_out) {
       // the largest magnitude of 128 columns, over the wavefronts that hold them
       __syncthreads();
@@ -496,8 +513,8 @@ __global__ __launch_bounds__(S::kThreads) void wb_linear_tile_kernel(LinearArgs 
         const RowScale q = row_scale(most);
         if (c == 0 && wn % span == 0) a.out_scales[m * a.ld_os + wave_col / kScaleBlock] = q.s;
         const f32x4 g = *reinterpret_cast<const f32x4*>(mine + r * kPitch + at);
-        float v[4];
-        for (int e = 0; e < 4; ++e) v[e] = quotient(g[e], q);
+        float v[4] = {g[0], g[1], g[2], g[3]};
+        quotients(v, q);
         store_four(a.out, m * a.ld_out + wave_col + c, WB_F8E4M3, in_row, v);
       }
     }
@@ -521,7 +538,7 @@ __global__ __launch_bounds__(256) void wb_linear_codes_kernel(const float* sums,
   for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(v[i]));
   const RowScale q = row_scale(reduce16(top, FMax()));
   if ((threadIdx.x & 15) == 0) a.out_scales[row * a.ld_os + c / kScaleBlock] = q.s;
-  for (int i = 0; i < 8; ++i) v[i] = quotient(v[i], q);
+  quotients(v, q);
   uint8_t* to = static_cast<uint8_t*>(a.out) + row * a.ld_out + c;
   const u32x2 p = {pack_fp8(v[0], v[1], v[2], v[3]), pack_fp8(v[4], v[5], v[6], v[7])};
   if (c + 8 <= a.n_out) {

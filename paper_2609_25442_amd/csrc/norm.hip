@@ -14,11 +14,14 @@ namespace wb {
 namespace {
 
 constexpr int kMaxWaves = 16;
+constexpr int64_t kManyRows = 2048;
 
 // A row takes `waves` wavefronts (ROWS > 1: one, and the workgroup holds ROWS
 // rows), each lane V runs of eight columns. LOOP: rows wider than the registers; the
-// second pass reads its operands again.
-template <int V, int ROWS, bool LOOP>
+// second pass reads its operands again. NT: more bytes than the caches keep
+// for the next reader, streamed past them (16384 x 7168 to fp8: 141 us against
+// 158; at 2048 rows 23 us against 21).
+template <int V, int ROWS, bool LOOP, bool NT>
 __global__ __launch_bounds__(ROWS > 1 ? 64 * ROWS : 64 * kMaxWaves) void wb_add_rms_norm_kernel(NormArgs a) {
   __shared__ float part[kMaxWaves];
   const int wave = threadIdx.x >> 6;
@@ -36,9 +39,9 @@ __global__ __launch_bounds__(ROWS > 1 ? 64 * ROWS : 64 * kMaxWaves) void wb_add_
   auto load = [&](int64_t c, float(&t)[8]) {
     float r[8];
     if (c + 8 <= a.cols) {
-      load_eight(x, c, a.x_type, t);
+      load_eight<NT>(x, c, a.x_type, t);
       if (!a.residual) return;
-      load_eight(res, c, a.residual_type, r);
+      load_eight<NT>(res, c, a.residual_type, r);
     } else {
       load_tail(x, c, a.cols, a.x_type, t);
       if (!a.residual) return;
@@ -85,7 +88,7 @@ __global__ __launch_bounds__(ROWS > 1 ? 64 * ROWS : 64 * kMaxWaves) void wb_add_
         if (c < a.cols) load(c, t[v]);
       }
       if (whole) {
-        if (a.total) store_eight(total, c, a.total_type, t[v]);
+        if (a.total) store_eight<NT>(total, c, a.total_type, t[v]);
         load_eight(a.weight, c, a.weight_type, y);
       } else {
         if (a.total) store_tail(total, c, a.cols, a.total_type, t[v]);
@@ -97,16 +100,16 @@ __global__ __launch_bounds__(ROWS > 1 ? 64 * ROWS : 64 * kMaxWaves) void wb_add_
         for (int i = 0; i < 8; ++i) amax = fmaxf(amax, fabsf(y[i]));
         const RowScale q = row_scale(reduce16(amax, FMax()));
         if ((lane & 15) == 0) a.scales[row * a.ld_scales + c / kScaleBlock] = q.s;
-        for (int i = 0; i < 8; ++i) y[i] = quotient(y[i], q);
+        quotients(y, q);
         const u32x2 p = {pack_fp8(y[0], y[1], y[2], y[3]), pack_fp8(y[4], y[5], y[6], y[7])};
         if (whole) {
-          *reinterpret_cast<u32x2_a1*>(out + c) = p;
+          put_u2<NT>(reinterpret_cast<u32x2_a1*>(out + c), p);
         } else {
           for (int i = 0; i < 8; ++i)
             if (c + i < a.cols) out[c + i] = static_cast<char>(p[i >> 2] >> (8 * (i & 3)));
         }
       } else if (whole) {
-        store_eight(out, c, a.out_type, y);
+        store_eight<NT>(out, c, a.out_type, y);
       } else {
         store_tail(out, c, a.cols, a.out_type, y);
       }
@@ -117,7 +120,12 @@ __global__ __launch_bounds__(ROWS > 1 ? 64 * ROWS : 64 * kMaxWaves) void wb_add_
 template <int V, int ROWS, bool LOOP>
 hipError_t launch(const NormArgs& a, int waves, hipStream_t st) {
   const dim3 grid(static_cast<uint32_t>((a.rows + ROWS - 1) / ROWS)), block(64 * (ROWS > 1 ? ROWS : waves));
-  hipLaunchKernelGGL((wb_add_rms_norm_kernel<V, ROWS, LOOP>), grid, block, 0, st, a);
+  const int64_t row_bytes = a.cols * (bytes_of(a.x_type) + (a.residual ? bytes_of(a.residual_type) : 0) +
+                                      (a.total ? bytes_of(a.total_type) : 0) + bytes_of(a.out_type));
+  if (a.rows * row_bytes > kStreamBytes)
+    hipLaunchKernelGGL((wb_add_rms_norm_kernel<V, ROWS, LOOP, true>), grid, block, 0, st, a);
+  else
+    hipLaunchKernelGGL((wb_add_rms_norm_kernel<V, ROWS, LOOP, false>), grid, block, 0, st, a);
   return hipGetLastError();
 }
 
@@ -126,13 +134,19 @@ hipError_t launch(const NormArgs& a, int waves, hipStream_t st) {
 int launch_add_rms_norm(const NormArgs& a, void* stream) {
   const auto st = static_cast<hipStream_t>(stream);
   if (a.rows == 0) return hipSuccess;
-  // narrow rows: one wavefront each, four to a workgroup; wider ones: as many
-  // wavefronts as give a lane two runs, or four; past that, two passes
+  // Narrow rows: one wavefront each, four to a workgroup. Wider ones: with
+  // many rows four runs a lane (16384 x 7168 to fp8: 141 us against 148 of two
+  // and 189 of one), one up to eight wavefronts (16384 x 4096 to bf16: 87 us
+  // against 90 of two and 97 of four); with few rows two, which gives a row
+  // more wavefronts (512 x 7168: 8.2 us against 10.2 of four). Past sixteen
+  // wavefronts of four, two passes.
   const int64_t runs = (a.cols + 7) / 8;
+  const auto waves = [&](int v) { return static_cast<int>((runs + 64 * v - 1) / (64 * v)); };
   if (runs <= 64) return launch<1, 4, false>(a, 1, st);
   if (runs <= 128) return launch<2, 4, false>(a, 1, st);
-  if (runs <= 128 * kMaxWaves) return launch<2, 1, false>(a, static_cast<int>((runs + 127) / 128), st);
-  if (runs <= 256 * kMaxWaves) return launch<4, 1, false>(a, static_cast<int>((runs + 255) / 256), st);
+  if (a.rows >= kManyRows && runs <= 512) return launch<1, 1, false>(a, waves(1), st);
+  if (a.rows < kManyRows && waves(2) <= kMaxWaves) return launch<2, 1, false>(a, waves(2), st);
+  if (waves(4) <= kMaxWaves) return launch<4, 1, false>(a, waves(4), st);
   return launch<4, 1, true>(a, kMaxWaves, st);
 }
 

@@ -31,6 +31,10 @@ __device__ __forceinline__ uint32_t pack_fp8(float a, float b, float c, float d)
   return static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(c, d, p, true));
 }
 
+constexpr int64_t kStreamBytes = int64_t(128) << 20;  // from here on a launch's data goes past the caches
+
+__host__ __device__ __forceinline__ int64_t bytes_of(int type) { return type == WB_F32 ? 4 : type == WB_BF16 ? 2 : 1; }
+
 // One element of a row.
 __device__ __forceinline__ float load_one(const void* row, int64_t col, int type) {
   return type == WB_F32 ? static_cast<const float*>(row)[col] : bf16_to_f32(static_cast<const uint16_t*>(row)[col]);
@@ -50,13 +54,42 @@ typedef u32x4 u32x4_a2 __attribute__((aligned(2)));
 typedef f32x4 f32x4_a4 __attribute__((aligned(4)));
 typedef u32x2 u32x2_a1 __attribute__((aligned(1)));
 
+// NT: with the non-temporal hint, for data that is touched once. (One function
+// a type: a template parameter would lose the type's alignment.)
+template <bool NT>
+__device__ __forceinline__ f32x4 get_f4(const f32x4_a4* p) { return NT ? __builtin_nontemporal_load(p) : *p; }
+template <bool NT>
+__device__ __forceinline__ u32x4 get_u4(const u32x4_a2* p) { return NT ? __builtin_nontemporal_load(p) : *p; }
+template <bool NT>
+__device__ __forceinline__ void put_f4(f32x4_a4* p, f32x4 v) {
+  if (NT)
+    __builtin_nontemporal_store(v, p);
+  else
+    *p = v;
+}
+template <bool NT>
+__device__ __forceinline__ void put_u4(u32x4_a2* p, u32x4 v) {
+  if (NT)
+    __builtin_nontemporal_store(v, p);
+  else
+    *p = v;
+}
+template <bool NT>
+__device__ __forceinline__ void put_u2(u32x2_a1* p, u32x2 v) {
+  if (NT)
+    __builtin_nontemporal_store(v, p);
+  else
+    *p = v;
+}
+
+template <bool NT = false>
 __device__ __forceinline__ void load_eight(const void* row, int64_t col, int type, float (&v)[8]) {
   if (type == WB_F32) {
     const auto* p = reinterpret_cast<const f32x4_a4*>(static_cast<const float*>(row) + col);
-    const f32x4 a = p[0], b = p[1];
+    const f32x4 a = get_f4<NT>(p), b = get_f4<NT>(p + 1);
     for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
   } else {
-    const u32x4 a = *reinterpret_cast<const u32x4_a2*>(static_cast<const uint16_t*>(row) + col);
+    const u32x4 a = get_u4<NT>(reinterpret_cast<const u32x4_a2*>(static_cast<const uint16_t*>(row) + col));
     for (int i = 0; i < 4; ++i) {
       v[2 * i] = __builtin_bit_cast(float, a[i] << 16);
       v[2 * i + 1] = __builtin_bit_cast(float, a[i] & 0xffff0000u);
@@ -79,14 +112,15 @@ __device__ __forceinline__ void load_tail(const void* row, int64_t col, int64_t 
   for (int i = 0; i < 8; ++i) v[i] = by >= 8 ? 0.0f : v[i];
 }
 
+template <bool NT = false>
 __device__ __forceinline__ void store_eight(void* row, int64_t col, int type, const float (&v)[8]) {
   if (type == WB_F32) {
     auto* p = reinterpret_cast<f32x4_a4*>(static_cast<float*>(row) + col);
-    p[0] = f32x4{v[0], v[1], v[2], v[3]};
-    p[1] = f32x4{v[4], v[5], v[6], v[7]};
+    put_f4<NT>(p, f32x4{v[0], v[1], v[2], v[3]});
+    put_f4<NT>(p + 1, f32x4{v[4], v[5], v[6], v[7]});
   } else {
-    *reinterpret_cast<u32x4_a2*>(static_cast<uint16_t*>(row) + col) =
-        u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+    put_u4<NT>(reinterpret_cast<u32x4_a2*>(static_cast<uint16_t*>(row) + col),
+               u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])});
   }
 }
 
@@ -95,16 +129,38 @@ __device__ __forceinline__ void store_tail(void* row, int64_t col, int64_t cols,
     if (col + i < cols) store_one(row, col + i, type, v[i]);
 }
 
-template <class Op>
-__device__ __forceinline__ float reduce16(float v, Op op) {
-  for (int off = 8; off > 0; off >>= 1) v = op(v, __shfl_xor(v, off, 16));
-  return v;
+// The sixteen lanes of a row, turned by N: every lane gets the result of a
+// reduction after N = 8, 4, 2, 1, in vector instructions alone.
+template <int N, class T>
+__device__ __forceinline__ T turned16(T v) {
+  const int i = __builtin_bit_cast(int, v);
+  return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(i, i, 0x120 + N, 0xf, 0xf, false));
 }
+
+template <class T, class Op>
+__device__ __forceinline__ T reduce16(T v, Op op) {
+  v = op(v, turned16<8>(v));
+  v = op(v, turned16<4>(v));
+  v = op(v, turned16<2>(v));
+  return op(v, turned16<1>(v));
+}
+
+// Between writes to LDS and reads of them by other lanes of the wavefront:
+// the hardware keeps their order, this keeps the compiler to it.
+__device__ __forceinline__ void order_lanes() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
 
 __device__ __forceinline__ float sum_of_wave(float v) {
   for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off);
   return v;
 }
+
+struct Sum {
+  __device__ __forceinline__ float operator()(float a, float b) const { return a + b; }
+};
+
+struct IMin {
+  __device__ __forceinline__ int operator()(int a, int b) const { return min(a, b); }
+};
 
 struct FMax {
   __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
@@ -128,10 +184,16 @@ __device__ __forceinline__ RowScale row_scale(float amax) {
 }
 
 // v / s rounded to fp32: one product, its remainder, one correction.
-__device__ __forceinline__ float quotient(float v, const RowScale& q) {
-  if (!q.near) return v / q.s;
-  const float a = v * q.r;
-  return __builtin_fmaf(__builtin_fmaf(-a, q.s, v), q.r, a);
+template <int N>
+__device__ __forceinline__ void quotients(float (&v)[N], const RowScale& q) {
+  if (q.near) {
+    for (int i = 0; i < N; ++i) {
+      const float a = v[i] * q.r;
+      v[i] = __builtin_fmaf(__builtin_fmaf(-a, q.s, v[i]), q.r, a);
+    }
+  } else {
+    for (int i = 0; i < N; ++i) v[i] /= q.s;
+  }
 }
 
 }  // namespace wb
