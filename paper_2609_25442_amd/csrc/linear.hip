@@ -11,6 +11,7 @@
 // the sums of a block are scaled and added in fp32.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "ops_device.hpp"
 
@@ -154,20 +155,6 @@ __device__ __forceinline__ void store_four(void* base, int64_t at, int type, int
   }
 }
 
-// What becomes of the sums of four columns from col on; u are the sums of the
-// up rows where the weight is gated. in_row: columns that exist (none for a
-// row past the end).
-__device__ __forceinline__ void finish(const LinearArgs& a, int expert, int col, int in_row, float (&v)[4], float (&u)[4]) {
-  if (a.bias && in_row > 0) {
-    for (int r = 0; r < 4; ++r) {
-      const int c = min(col + r, a.n_out - 1);
-      v[r] += load_bias(a, expert, c);
-      if (a.gated) u[r] += load_bias(a, expert, a.n_out + c);
-    }
-  }
-  for (int r = 0; r < 4; ++r) v[r] = a.gated ? activate(v[r], a.activation) * u[r] : activate(v[r], a.activation);
-}
-
 __device__ __forceinline__ float largest(const float (&v)[4], int in_row, float top) {
   for (int r = 0; r < 4; ++r)
     if (r < in_row) top = fmaxf(top, fabsf(v[r]));
@@ -206,7 +193,7 @@ struct Operand {
 // The same rows of the weight against M blocks of tokens: the sums of one
 // block depend on each other, those of different blocks do not.
 template <bool F8, int M>
-__device__ __forceinline__ void block_sums(const Operand<F8>& w, const Operand<F8> (&x)[M], f32x4 (&c)[M]) {
+__device__ __forceinline__ void block_sums(const Operand<F8>& w, const Operand<F8>* x, f32x4* c) {
 #pragma unroll
   for (int h = 0; h < (F8 ? 4 : 2); ++h)
 #pragma unroll
@@ -241,7 +228,7 @@ __device__ __forceinline__ int swizzle(int row) { return (row >> 1) & 7; }
 // scale: tiles go from memory to LDS without registers between. Otherwise
 // through registers, piece by piece, and scales by row.
 template <class S, bool F8, bool DIRECT>
-__global__ __launch_bounds__(S::kThreads) void wb_linear_tile_kernel(LinearArgs a, uint32_t tiles_n, uint32_t group) {
+__global__ __launch_bounds__(S::kThreads, 2) void wb_linear_tile_kernel(LinearArgs a, uint32_t tiles_n, uint32_t group) {
   extern __shared__ __align__(128) uint8_t lds[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int kg = wave / (S::WM * S::WN), wm = wave / S::WN % S::WM, wn = wave % S::WN;
@@ -271,16 +258,30 @@ __global__ __launch_bounds__(S::kThreads) void wb_linear_tile_kernel(LinearArgs 
   constexpr int kWaves = S::kThreads / 64, kPieces = S::kRows * S::STEP * 8 / S::kThreads;  // per lane and step
   static_assert(kWaves % 2 == 0, "the pieces of a lane are permuted alike");
   const int piece = ((lane & 7) ^ swizzle(wave * 8 + (lane >> 3))) * 16;
-  const uint8_t* src[kPieces];
-  u32x4 held[DIRECT ? 1 : kPieces];
+  // DIRECT keeps a piece as its 32-bit offset from the weight or from x (the
+  // tile's first row, where rows are not gathered), which the loads add to an
+  // address that is the same for the wavefront; the launch sees to its range
+  const uint8_t* const x_base = a.tokens ? a.x : a.x + rows.first * a.ld_x_bytes;
+  const uint8_t* src[DIRECT ? 1 : kPieces];
+  uint32_t off[DIRECT ? kPieces : 1];
+  constexpr bool kApart = S::STEP == 1 && S::BN % (kWaves * 8) == 0;  // the weight's pieces come first, in every wavefront
+  auto of_weight = [&](int i) { return kApart ? i * kWaves * 8 < S::BN : (wave + i * kWaves) * 8 % S::kRows < S::BN; };
 #pragma unroll
   for (int i = 0; i < kPieces; ++i) {
     const int r = (wave + i * kWaves) * 8;  // of the step's rows; its stage is the same for the wavefront
-    src[i] = row_of(r % S::kRows + (lane >> 3)) + r / S::kRows * kStageBytes;
+    const uint8_t* from = row_of(r % S::kRows + (lane >> 3)) + r / S::kRows * kStageBytes;
+    if constexpr (DIRECT)
+      off[i] = static_cast<uint32_t>(from - (of_weight(i) ? weight : x_base)) + piece;
+    else
+      src[i] = from;
   }
   // scales: a row of x, then of the weight, per thread and round
   const float* scale_src[S::kRounds];
-  float scale_held[S::kRounds];
+  // otherwise two steps' pieces and scales are in registers on their way
+  struct Held {
+    u32x4 piece[DIRECT ? 1 : kPieces];
+    float scale[S::kRounds];
+  };
   uint8_t* const scales = lds + S::RING * S::kSlot;
   if constexpr (F8) {
 #pragma unroll
@@ -292,63 +293,83 @@ __global__ __launch_bounds__(S::kThreads) void wb_linear_tile_kernel(LinearArgs 
     }
   }
 
-  // start step t's stages on their way into a slot of the ring: DIRECT, all
-  // the way. Stages past the end are zeros.
-  int put_at = 0;
-  auto fetch = [&](int t, int slot) {
-    put_at = slot;
-    const int64_t at = int64_t(t) * (S::STEP * kStageBytes) + piece;
-    const bool whole = (t + 1) * int64_t(S::STEP * kStageBytes) <= k_bytes;
+  // the scale of a step that thread and round have to bring
+  auto scale_at = [&](int t, int i) {
+    const int h = min(tid + i * S::kThreads, S::STEP * S::kRows - 1) / S::kRows;
+    return scale_src[i] + min(t * S::STEP + h, stages - 1);
+  };
+  auto send_scales = [&](int t, int slot) {
     if constexpr (F8) {
 #pragma unroll
-      for (int i = 0; i < S::kRounds; ++i) {
-        const int h = min(tid + i * S::kThreads, S::STEP * S::kRows - 1) / S::kRows;
-        const float* p = scale_src[i] + min(t * S::STEP + h, stages - 1);
-        if constexpr (DIRECT)
-          __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p,
-                                           (__attribute__((address_space(3))) void*)(scales + slot * S::kScales + (wave * 64 + i * S::kThreads) * 4),
-                                           4, 0, 0);
-        else
-          scale_held[i] = *p;
-      }
+      for (int i = 0; i < S::kRounds; ++i)
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)scale_at(t, i),
+                                         (__attribute__((address_space(3))) void*)(scales + slot * S::kScales + (wave * 64 + i * S::kThreads) * 4),
+                                         4, 0, 0);
     }
+  };
+  auto send = [&](const uint8_t* p, int slot, int i) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p,
+                                     (__attribute__((address_space(3))) void*)(lds + slot * S::kSlot + (wave + i * kWaves) * 1024), 16, 0, 0);
+  };
+  struct At {  // where a step lies in every row
+    const uint8_t *weight, *x;
+  };
+  auto step_at = [&](int t) {
+    return At{weight + int64_t(t) * (S::STEP * kStageBytes), x_base + int64_t(t) * (S::STEP * kStageBytes)};
+  };
+  // piece i of a step that lies within k
+  auto send_whole = [&](const At& at, int slot, int i) {
+    if constexpr (DIRECT) send((of_weight(i) ? at.weight : at.x) + off[i], slot, i);
+  };
+  // start step t's stages on their way into a slot of the ring; stages past
+  // the end are zeros
+  auto fetch = [&](int t, int slot) {
     if constexpr (DIRECT) {
-      uint8_t* to = lds + slot * S::kSlot + wave * 1024;
-      auto load = [&](const uint8_t* p, int i) {
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p,
-                                         (__attribute__((address_space(3))) void*)(to + i * kWaves * 1024), 16, 0, 0);
-      };
-      if (whole) {
+      send_scales(t, slot);
+      const At from = step_at(t);
+      if ((t + 1) * int64_t(S::STEP * kStageBytes) <= k_bytes) {
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) load(src[i] + at, i);
+        for (int i = 0; i < kPieces; ++i) send_whole(from, slot, i);
       } else {
+        const int64_t at = int64_t(t) * (S::STEP * kStageBytes) + piece;
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
-          const int64_t from = at + (wave + i * kWaves) * 8 / S::kRows * kStageBytes;
-          load(from < k_bytes ? src[i] + at : reinterpret_cast<const uint8_t*>(&zero_piece), i);
+          const int64_t in_row = at + (wave + i * kWaves) * 8 / S::kRows * kStageBytes;
+          const uint8_t* p = (of_weight(i) ? from.weight : from.x) + off[i];
+          send(in_row < k_bytes ? p : reinterpret_cast<const uint8_t*>(&zero_piece), slot, i);
         }
-      }
-    } else if (whole) {
-#pragma unroll
-      for (int i = 0; i < kPieces; ++i) held[i] = *reinterpret_cast<const u32x4_a1*>(src[i] + at);
-    } else {
-#pragma unroll
-      for (int i = 0; i < kPieces; ++i) {
-        const int stage = (wave + i * kWaves) * 8 / S::kRows * kStageBytes;
-        held[i] = load_piece(src[i] - stage, at + stage, k_bytes);
       }
     }
   };
-  // not DIRECT: what fetch() left in registers goes into its slot
-  auto put = [&]() {
+  // the same by way of registers
+  auto take = [&](int t, Held& held) {
     if constexpr (!DIRECT) {
-      uint8_t* to = lds + put_at * S::kSlot + wave * 1024 + lane * 16;
+      const int64_t at = int64_t(t) * (S::STEP * kStageBytes) + piece;
+      if ((t + 1) * int64_t(S::STEP * kStageBytes) <= k_bytes) {
 #pragma unroll
-      for (int i = 0; i < kPieces; ++i) *reinterpret_cast<u32x4*>(to + i * kWaves * 1024) = held[i];
+        for (int i = 0; i < kPieces; ++i) held.piece[i] = *reinterpret_cast<const u32x4_a1*>(src[i] + at);
+      } else {
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+          const int stage = (wave + i * kWaves) * 8 / S::kRows * kStageBytes;
+          held.piece[i] = load_piece(src[i] - stage, at + stage, k_bytes);
+        }
+      }
+      if constexpr (F8) {
+#pragma unroll
+        for (int i = 0; i < S::kRounds; ++i) held.scale[i] = *scale_at(t, i);
+      }
+    }
+  };
+  auto put = [&](const Held& held, int slot) {
+    if constexpr (!DIRECT) {
+      uint8_t* to = lds + slot * S::kSlot + wave * 1024 + lane * 16;
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i) *reinterpret_cast<u32x4*>(to + i * kWaves * 1024) = held.piece[i];
       if constexpr (F8) {
 #pragma unroll
         for (int i = 0; i < S::kRounds; ++i)
-          *reinterpret_cast<float*>(scales + put_at * S::kScales + (tid + i * S::kThreads) * 4) = scale_held[i];
+          *reinterpret_cast<float*>(scales + slot * S::kScales + (tid + i * S::kThreads) * 4) = held.scale[i];
       }
     }
   };
@@ -362,22 +383,11 @@ __global__ __launch_bounds__(S::kThreads) void wb_linear_tile_kernel(LinearArgs 
   const int frag = l15 * kStageBytes + ((quad ^ swizzle(l15)) << 4);
   const int w_frag = wn * S::TN * kStageBytes + frag, x_frag = (S::BN + wm * S::TM) * kStageBytes + frag;
 
-  // DIRECT keeps RING - 1 steps in flight, the other way one
-  constexpr int kAhead = DIRECT ? S::RING - 1 : 1;
-  constexpr int kLoads = kPieces + (F8 ? S::kRounds : 0);  // of a wavefront and step
-  static_assert(!DIRECT || (kAhead - 1) * kLoads < 64, "the counter of loads in flight");
   const int steps = (stages + S::STEP - 1) / S::STEP;
-  for (int t = 0; t < min(kAhead, steps); ++t) fetch(t, t);
-  put();
-  int slot = 0;
-  for (int t = 0; t < steps; ++t) {
-    // after this, step t is in LDS for every wavefront, and the step before it
-    // has been read by all: its slot can be filled
-    if (DIRECT && t + kAhead <= steps)
-      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((kAhead - 1) * kLoads) : "memory");
-    else
-      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (t + kAhead < steps) fetch(t + kAhead, slot + kAhead >= S::RING ? slot + kAhead - S::RING : slot + kAhead);
+
+  // the products of the stages in a slot, `between` in front of each block of
+  // sixteen rows of the weight
+  auto compute = [&](int slot, auto&& between) {
 #pragma unroll
     for (int h = 0; h < S::STEP / S::KG; ++h) {
     const int stage = h * S::KG + kg;
@@ -386,6 +396,7 @@ __global__ __launch_bounds__(S::kThreads) void wb_linear_tile_kernel(LinearArgs 
     auto operand = [&](int at) {
       return Operand<F8>(*reinterpret_cast<const i32x4*>(buf + at), *reinterpret_cast<const i32x4*>(buf + (at ^ 64)));
     };
+    constexpr int kTogether = S::FM < 2 ? 1 : 2;  // chains of products that do not wait for each other
     Operand<F8> x[S::FM];
     float sx[S::FM];
 #pragma unroll
@@ -395,30 +406,86 @@ __global__ __launch_bounds__(S::kThreads) void wb_linear_tile_kernel(LinearArgs 
     }
 #pragma unroll
     for (int i = 0; i < S::FN; ++i) {
+      between(h * S::FN + i);
       const Operand<F8> w = operand(w_frag + i * 16 * kStageBytes);
       if constexpr (F8) {
         const float* sw = sc + S::BM + wn * S::TN + i * 16;
         const f32x4 sr = DIRECT ? f32x4{sw[0], sw[0], sw[0], sw[0]} : *reinterpret_cast<const f32x4*>(sw + quad * 4);
-        f32x4 part[S::FM];
 #pragma unroll
-        for (int j = 0; j < S::FM; ++j) part[j] = f32x4{0, 0, 0, 0};
-        block_sums<F8>(w, x, part);
+        for (int j0 = 0; j0 < S::FM; j0 += kTogether) {
+          f32x4 part[kTogether];
 #pragma unroll
-        for (int j = 0; j < S::FM; ++j) {
-          if constexpr (DIRECT) {
-            const float both = sx[j] * sr[0];
-            for (int r = 0; r < 4; ++r) acc[i][j][r] = __builtin_fmaf(part[j][r], both, acc[i][j][r]);
-          } else {
-            for (int r = 0; r < 4; ++r) acc[i][j][r] = __builtin_fmaf(part[j][r], sx[j] * sr[r], acc[i][j][r]);
+          for (int j = 0; j < kTogether; ++j) part[j] = f32x4{0, 0, 0, 0};
+          block_sums<F8, kTogether>(w, x + j0, part);
+#pragma unroll
+          for (int j = 0; j < kTogether; ++j) {
+            f32x4& to = acc[i][j0 + j];
+            if constexpr (DIRECT) {
+              const float both = sx[j0 + j] * sr[0];
+              for (int r = 0; r < 4; ++r) to[r] = __builtin_fmaf(part[j][r], both, to[r]);
+            } else {
+              for (int r = 0; r < 4; ++r) to[r] = __builtin_fmaf(part[j][r], sx[j0 + j] * sr[r], to[r]);
+            }
           }
         }
       } else {
-        block_sums<F8>(w, x, acc[i]);
+        block_sums<F8, S::FM>(w, x, acc[i]);
       }
     }
     }
-    slot = slot + 1 == S::RING ? 0 : slot + 1;
-    if (t + 1 < steps) put();
+  };
+  if constexpr (DIRECT) {
+    constexpr int kBlocks = S::STEP / S::KG * S::FN;                    // calls of `between`
+    constexpr int kAhead = S::RING - 1;                                 // steps in flight
+    constexpr int kLoads = kPieces + (F8 ? S::kRounds : 0);             // of a wavefront and step
+    static_assert((kAhead - 1) * kLoads < 64, "the counter of loads in flight");
+    auto next = [](int slot, int by) { return slot + by >= S::RING ? slot + by - S::RING : slot + by; };
+    int slot = 0, t = 0;
+    for (int i = 0; i < min(kAhead, steps); ++i) fetch(i, i);
+    // As long as the step to fetch lies within k, its loads go out one by one
+    // between the products: issued together, they hold up the matrix cores
+    // (8192 x 8192 x 8192 bf16: 10 % of the time).
+    const int whole_steps = static_cast<int>(k_bytes / (S::STEP * kStageBytes));
+    for (; t + kAhead < whole_steps; ++t) {
+      // after this, step t is in LDS for every wavefront, and the step before
+      // it has been read by all: its slot can be filled
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((kAhead - 1) * kLoads) : "memory");
+      const int to = next(slot, kAhead);
+      const At from = step_at(t + kAhead);
+      send_scales(t + kAhead, to);
+      compute(slot, [&](int block) {
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i)
+          if (i * kBlocks / kPieces == block) send_whole(from, to, i);
+      });
+      slot = next(slot, 1);
+    }
+    for (; t < steps; ++t) {
+      if (t + kAhead <= steps)
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((kAhead - 1) * kLoads) : "memory");
+      else
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      if (t + kAhead < steps) fetch(t + kAhead, next(slot, kAhead));
+      compute(slot, [](int) {});
+      slot = next(slot, 1);
+    }
+  } else {
+    // step t is in slot t % 2, step t + 1 in registers when the barrier in
+    // front of step t is passed, and step t + 2 then sets out
+    Held even, odd;
+    auto one = [&](int t, const Held& ready, Held& free) {
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      if (t + 2 < steps) take(t + 2, free);
+      compute(t & 1, [](int) {});
+      if (t + 1 < steps) put(ready, (t + 1) & 1);
+    };
+    take(0, even);
+    if (steps > 1) take(1, odd);
+    put(even, 0);
+    for (int t = 0; t < steps; t += 2) {
+      one(t, odd, even);
+      if (t + 1 < steps) one(t + 1, even, odd);
+    }
   }
 
   if constexpr (S::KG > 1) {
@@ -453,69 +520,94 @@ __global__ __launch_bounds__(S::kThreads) void wb_linear_tile_kernel(LinearArgs 
   float* const mine = reinterpret_cast<float*>(lds) + wave % (S::WM * S::WN) * 16 * kPitch;
   float* const tops = reinterpret_cast<float*>(scales);
   const int cols = a.gated ? S::TN / 2 : S::TN, lanes = cols / 4, span = kScaleBlock / cols;
-  const int wave_col = col0 + wn * cols, c = lane % lanes * 4, per = 64 / lanes;
+  const int wave_col = col0 + wn * cols, c = lane % lanes * 4, per = 64 / lanes, col = wave_col + c;
   const int at = a.gated ? (c >> 4) * 32 + (c & 15) : c;
-  const int in_row = a.n_out - (wave_col + c), first_r = kg == 0 ? lane / lanes : 16;
+  const int in_row = a.n_out - col, first_r = kg == 0 ? lane / lanes : 16;
   const bool f8_out = a.out_type == WB_F8E4M3;
-  __syncthreads();
-#pragma unroll
-  for (int j = 0; j < S::FM; ++j) {
-    if (kg == 0) {
-#pragma unroll
-      for (int i = 0; i < S::FN; ++i) *reinterpret_cast<f32x4*>(mine + l15 * kPitch + i * 16 + quad * 4) = acc[i][j];
+  const int64_t m0 = rows.first + wm * S::TM;
+  const int there = static_cast<int>(min(rows.end - m0, int64_t(S::TM)));  // rows of the wavefront that exist
+  float bias[4] = {0, 0, 0, 0}, bias_up[4] = {0, 0, 0, 0};
+  if (a.bias && in_row > 0) {
+    for (int e = 0; e < 4; ++e) {
+      const int b = min(col + e, a.n_out - 1);
+      bias[e] = load_bias(a, rows.expert, b);
+      if (a.gated) bias_up[e] = load_bias(a, rows.expert, a.n_out + b);
     }
-    order_lanes();
-    // four of the lane's rows at a time, so that their residuals' loads overlap
+  }
+  // Four of the lane's rows of block j at a time. The residual's loads come
+  // first, and only where there is one: a wait for loads is one for the
+  // stores before them as well.
+  auto finish_rows = [&](int j, auto with_residual) {
 #pragma unroll 1
     for (int r0 = first_r; r0 < 16; r0 += 4 * per) {
       float add[4][4];
+      if constexpr (with_residual) {
 #pragma unroll
-      for (int h = 0; h < 4; ++h) {
-        const int64_t m = rows.first + wm * S::TM + j * 16 + r0 + h * per;
-        if (a.residual && r0 + h * per < 16 && m < rows.end && in_row > 0)
-          load_four(a.residual, m * a.ld_residual + wave_col + c, a.residual_type, in_row, add[h]);
-        else
-          for (int e = 0; e < 4; ++e) add[h][e] = 0.0f;
+        for (int h = 0; h < 4; ++h) {
+          const int r = j * 16 + r0 + h * per;
+          load_four(a.residual, (m0 + min(r, there - 1)) * a.ld_residual + col, a.residual_type, in_row, add[h]);
+        }
       }
 #pragma unroll
       for (int h = 0; h < 4; ++h) {
         const int r = r0 + h * per;
         if (r >= 16) break;
-        const int64_t m = rows.first + wm * S::TM + j * 16 + r;
-        const int in = m < rows.end ? in_row : 0;
+        const int in = j * 16 + r < there ? in_row : 0;
         float* p = mine + r * kPitch + at;
         const f32x4 g = *reinterpret_cast<const f32x4*>(p);
-        const f32x4 w = a.gated ? *reinterpret_cast<const f32x4*>(p + 16) : g;
-        float v[4] = {g[0], g[1], g[2], g[3]}, u[4] = {w[0], w[1], w[2], w[3]};
-        finish(a, rows.expert, wave_col + c, in, v, u);
-        for (int e = 0; e < 4; ++e) v[e] += add[h][e];
+        float v[4];
+        if (a.gated) {
+          const f32x4 u = *reinterpret_cast<const f32x4*>(p + 16);
+          for (int e = 0; e < 4; ++e) v[e] = activate(g[e] + bias[e], a.activation) * (u[e] + bias_up[e]);
+        } else {
+          for (int e = 0; e < 4; ++e) v[e] = activate(g[e] + bias[e], a.activation);
+        }
+        if constexpr (with_residual)
+          for (int e = 0; e < 4; ++e) v[e] += add[h][e];
         if (f8_out) {
           *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
           float top = largest(v, in, 0.0f);
           for (int off = lanes / 2; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
           if (c == 0) tops[wn * S::BM + wm * S::TM + j * 16 + r] = top;
         } else if (in > 0) {
-          store_four(a.out, m * a.ld_out + wave_col + c, a.out_type, in, v);
+          store_four(a.out, (m0 + j * 16 + r) * a.ld_out + col, a.out_type, in, v);
         }
       }
     }
+  };
+  __syncthreads();
+#pragma unroll 1
+  for (int j = 0; j < S::FM; ++j) {
+    if (kg == 0) {
+#pragma unroll
+      for (int k = 0; k < S::FM; ++k)
+        if (k == j) {  // a register has no index
+#pragma unroll
+          for (int i = 0; i < S::FN; ++i) *reinterpret_cast<f32x4*>(mine + l15 * kPitch + i * 16 + quad * 4) = acc[i][k];
+        }
+    }
+    order_lanes();
+    if (a.residual && there > 0)  // the same for the wavefront: lanes exchange maxima within
+      finish_rows(j, std::true_type());
+    else if (!a.residual || f8_out)
+      finish_rows(j, std::false_type());
     order_lanes();
     if (f8_out) {
       // the largest magnitude of 128 columns, over the wavefronts that hold them
       __syncthreads();
 #pragma unroll 1
       for (int r = first_r; r < 16; r += per) {
-        const int64_t m = rows.first + wm * S::TM + j * 16 + r;
-        if (m >= rows.end || in_row <= 0) continue;
+        if (j * 16 + r >= there || in_row <= 0) continue;
         float most = 0.0f;
         for (int w = wn / span * span; w < wn / span * span + span; ++w)
           most = fmaxf(most, tops[w * S::BM + wm * S::TM + j * 16 + r]);
         const RowScale q = row_scale(most);
+        const int64_t m = m0 + j * 16 + r;
         if (c == 0 && wn % span == 0) a.out_scales[m * a.ld_os + wave_col / kScaleBlock] = q.s;
         const f32x4 g = *reinterpret_cast<const f32x4*>(mine + r * kPitch + at);
         float v[4] = {g[0], g[1], g[2], g[3]};
         quotients(v, q);
-        store_four(a.out, m * a.ld_out + wave_col + c, WB_F8E4M3, in_row, v);
+        store_four(a.out, m * a.ld_out + col, WB_F8E4M3, in_row, v);
       }
     }
   }
@@ -573,40 +665,49 @@ hipError_t launch_tile(const LinearArgs& a, hipStream_t st) {
 
 
 // The tiles in use. A launch takes the one whose rounds over the 256 CUs are
-// expected to be done first: rounds * us, the measured time of a round per
-// stage of k with every CU busy, for bf16 and for fp8 (twice the k in a
-// stage), `resident` workgroups share a
-// CU, which pays from 256 tiles on: us_few holds for fewer. Large tiles read
-// less per product; small ones give every CU work, and more of them: for 333 x
-// 3456 x 1536 in bf16 64 x 64 takes 13 us and 256 x 256 50, for 8192 x 8192 x
-// 8192 1.66 ms and 0.89.
+// expected to be done first. A round takes us per stage of k (128 bytes of a
+// row) and `fixed` for its start and its results; `resident` workgroups share
+// a CU. Measured with 1024 tiles, and with 256 (`few`: up to there every tile
+// has a CU to itself), for bf16 and fp8; the last two are us, with 512 and
+// with 256 tiles, of rows that come by way of registers (0: not in use). Large
+// tiles read less per product; small ones give every CU work, and keep more of
+// the weight on its way when few rows meet it. 8192 x 8192 x 8192 bf16: 0.84
+// ms with 256 x 256, 0.95 with 128 x 128; 1024 x 7168 x 2048 fp8: 77 us and 43;
+// one row by 6144 x 4096 bf16: 12 us with 16 x 32, 31 with 64 x 64.
 struct Choice {
   int bm, bn, resident;
-  bool direct_only;
-  float us[2], us_few[2];  // bf16, fp8
+  float us[2], fixed, few_us[2], few_fixed;
+  float by_registers[2], few_by_registers[2];
 };
 constexpr Choice kChoices[] = {
-    {16, 32, 1, true, {0.14f, 0.17f}, {0.14f, 0.17f}},   {32, 32, 1, false, {0.18f, 0.21f}, {0.18f, 0.21f}},
-    {32, 64, 1, true, {0.25f, 0.32f}, {0.25f, 0.32f}},   {64, 64, 2, false, {0.56f, 0.74f}, {0.50f, 0.52f}},
-    {64, 64, 1, true, {0.33f, 0.49f}, {0.33f, 0.49f}},   {128, 64, 1, true, {0.46f, 0.83f}, {0.46f, 0.83f}},
-    {128, 128, 2, false, {1.18f, 2.25f}, {1.00f, 1.50f}}, {128, 128, 1, true, {0.86f, 1.25f}, {0.86f, 1.25f}},
-    {256, 256, 1, true, {1.72f, 3.90f}, {1.72f, 3.90f}},
+    {16, 32, 2, {0.105f, 0.137f}, 3.9f, {0.057f, 0.085f}, 4.8f, {}, {}},
+    {32, 32, 1, {0.075f, 0.129f}, 3.2f, {0.075f, 0.128f}, 4.4f, {0.264f, 0.358f}, {0.264f, 0.358f}},
+    {32, 64, 2, {0.28f, 0.437f}, 3.0f, {0.129f, 0.251f}, 4.3f, {}, {}},
+    {64, 64, 2, {0.43f, 0.645f}, 2.0f, {0.25f, 0.333f}, 6.0f, {0.78f, 1.82f}, {0.54f, 0.77f}},
+    {64, 64, 1, {0.22f, 0.345f}, 2.0f, {0.162f, 0.334f}, 6.0f, {}, {}},
+    {128, 64, 1, {0.355f, 0.632f}, 2.5f, {0.396f, 0.635f}, 3.0f, {1.0f, 1.5f}, {1.0f, 1.5f}},
+    {128, 128, 2, {0.95f, 1.8f}, 6.5f, {0.87f, 1.0f}, 5.0f, {1.72f, 0.0f}, {1.71f, 0.0f}},
+    {128, 128, 1, {0.655f, 0.90f}, 5.0f, {0.74f, 0.914f}, 6.0f, {}, {}},
+    {256, 256, 1, {1.5f, 3.24f}, 14.5f, {1.65f, 3.31f}, 11.5f, {}, {}},
 };
 constexpr int kNumChoices = sizeof(kChoices) / sizeof(kChoices[0]);
 
 int choose(const LinearArgs& a) {
   const int f8 = a.in_type == WB_F8E4M3;
+  const double stages = std::ceil(double(a.k) * (f8 ? 1 : 2) / kStageBytes);
   int best = -1;
   double least = 0.0;
   for (int i = 0; i < kNumChoices; ++i) {
     const Choice& c = kChoices[i];
-    if (c.direct_only && !a.direct) continue;
+    if (!a.direct && c.by_registers[f8] == 0.0f) continue;
     const int step = a.gated ? c.bn / 2 : c.bn;
     // of the experts' last tiles about half are empty
     double tiles_m = double(row_tiles(a, c.bm));
     if (a.offsets) tiles_m = std::min(double(a.rows), double(a.rows) / c.bm + 0.5 * std::min<int64_t>(a.num_experts, a.rows));
     const double tiles = tiles_m * ((a.n_out + step - 1) / step);
-    const double us = tiles <= 256 ? c.us_few[f8] : std::ceil(tiles / (256.0 * c.resident)) * c.us[f8];
+    const bool few = tiles <= 256;
+    const float per = a.direct ? (few ? c.few_us : c.us)[f8] : (few ? c.few_by_registers : c.by_registers)[f8];
+    const double us = (per * stages + (few ? c.few_fixed : c.fixed)) * (few ? 1.0 : std::ceil(tiles / (256.0 * c.resident)));
     if (best < 0 || us < least) best = i, least = us;
   }
   return best;
@@ -617,25 +718,32 @@ bool holds_scales(const LinearArgs& a, int choice) {
   return (a.gated ? kChoices[choice].bn / 2 : kChoices[choice].bn) % kScaleBlock == 0;
 }
 
-template <class S, bool ANY>
+template <class S, int CHOICE>
 hipError_t launch_shape(const LinearArgs& a, hipStream_t st) {
-  if constexpr (ANY) {
-    if (!a.direct) return a.in_type == WB_F8E4M3 ? launch_tile<S, true, false>(a, st) : launch_tile<S, false, false>(a, st);
+  constexpr Choice c = kChoices[CHOICE];
+  static_assert(c.bm == S::BM && c.bn == S::BN, "the tile of the table");
+  const bool f8 = a.in_type == WB_F8E4M3;
+  if (a.direct) return f8 ? launch_tile<S, true, true>(a, st) : launch_tile<S, false, true>(a, st);
+  if constexpr (c.by_registers[1] > 0.0f) {
+    if (f8) return launch_tile<S, true, false>(a, st);
   }
-  return a.in_type == WB_F8E4M3 ? launch_tile<S, true, true>(a, st) : launch_tile<S, false, true>(a, st);
+  if constexpr (c.by_registers[0] > 0.0f) {
+    if (!f8) return launch_tile<S, false, false>(a, st);
+  }
+  return hipErrorInvalidConfiguration;  // not chosen
 }
 
 hipError_t launch_choice(const LinearArgs& a, int choice, hipStream_t st) {
   switch (choice) {
-    case 0: return launch_shape<Shape<16, 32, 1, 1, 4, 4, 4>, false>(a, st);
-    case 1: return launch_shape<Shape<32, 32, 2, 1, 4, 4, 4>, true>(a, st);
-    case 2: return launch_shape<Shape<32, 64, 2, 2, 2, 4, 3>, false>(a, st);
-    case 3: return launch_shape<Shape<64, 64, 2, 2, 2, 2, 2>, true>(a, st);
-    case 4: return launch_shape<Shape<64, 64, 2, 2, 2, 2, 4>, false>(a, st);
-    case 5: return launch_shape<Shape<128, 64, 4, 2, 1, 2, 3>, false>(a, st);
-    case 6: return launch_shape<Shape<128, 128, 2, 2, 1, 1, 2>, true>(a, st);
-    case 7: return launch_shape<Shape<128, 128, 2, 2, 2, 2, 2>, false>(a, st);
-    default: return launch_shape<Shape<256, 256, 4, 2, 1, 1, 2>, false>(a, st);
+    case 0: return launch_shape<Shape<16, 32, 1, 1, 4, 4, 3>, 0>(a, st);
+    case 1: return launch_shape<Shape<32, 32, 2, 1, 4, 4, 4>, 1>(a, st);
+    case 2: return launch_shape<Shape<32, 64, 2, 2, 2, 2, 3>, 2>(a, st);
+    case 3: return launch_shape<Shape<64, 64, 2, 2, 2, 2, 2>, 3>(a, st);
+    case 4: return launch_shape<Shape<64, 64, 2, 2, 2, 2, 4>, 4>(a, st);
+    case 5: return launch_shape<Shape<128, 64, 4, 2, 1, 2, 3>, 5>(a, st);
+    case 6: return launch_shape<Shape<128, 128, 2, 2, 1, 1, 2>, 6>(a, st);
+    case 7: return launch_shape<Shape<128, 128, 2, 2, 2, 2, 2>, 7>(a, st);
+    default: return launch_shape<Shape<256, 256, 4, 2, 1, 1, 2>, 8>(a, st);
   }
 }
 

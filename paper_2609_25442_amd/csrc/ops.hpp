@@ -90,7 +90,9 @@ struct LinearArgs {
   int32_t k;
   int32_t in_type, bias_type, residual_type, out_type, activation;
   bool gated;
-  bool direct;  // rows of x and weight start at multiples of 16 bytes and hold a multiple of 16 bytes
+  // rows of x and weight start at multiples of 16 bytes and hold a multiple of
+  // 16, 32-bit offsets reach them, and sixteen rows of the weight share a scale
+  bool direct;
 };
 
 size_t route_workspace_bytes(int64_t rows, int32_t experts);

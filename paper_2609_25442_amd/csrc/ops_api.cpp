@@ -168,7 +168,10 @@ int check_linear(const wb_linear_args* p, Operands& ops, wb::LinearArgs& a) {
   const uintptr_t at = reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.weight) |
                        static_cast<uintptr_t>(a.ld_x_bytes) | static_cast<uintptr_t>(a.ld_w_bytes) |
                        static_cast<uintptr_t>(k * es);
-  a.direct = at % 16 == 0 && !(f8 && a.gated && n_out % 16 != 0);
+  // the kernels' offsets from the weight and from x have 32 bits
+  const int64_t reach = (int64_t(1) << 32) - 4096;
+  const bool near = n * a.ld_w_bytes < reach && (a.tokens ? a.x_rows : 256) * a.ld_x_bytes < reach;
+  a.direct = at % 16 == 0 && near && !(f8 && a.gated && n_out % 16 != 0);
   return WB_OK;
 }
 
