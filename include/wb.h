@@ -648,8 +648,8 @@ typedef struct wb_linear_args {
 } wb_linear_args;
 /* `workspace` (16-byte aligned, free again when the call's work is done) holds
  * the fp32 rows of some fp8 results; wb_linear_workspace says how many bytes
- * the same arguments need, 0 for most (then it may be NULL). Its errors are
- * those of wb_linear, WB_ESIZE aside. */
+ * the same arguments need, 0 for most (then it may be NULL). It does not look
+ * the pointers up. */
 int wb_linear_workspace(const wb_linear_args* args, size_t* bytes);
 int wb_linear(const wb_linear_args* args, void* workspace, size_t workspace_bytes, void* stream);
 

@@ -90,6 +90,15 @@ const Tensor& plain(const Tensor& t, at::ScalarType type, int64_t count, const c
   return t;
 }
 
+// One of the tensors that lie one after the other in `base`.
+Tensor part(const Tensor& base, int64_t& at, at::IntArrayRef shape) {
+  Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(base.storage()), base.key_set(), base.dtype());
+  t.unsafeGetTensorImpl()->set_storage_offset(base.storage_offset() + at);
+  t.unsafeGetTensorImpl()->set_sizes_contiguous(shape);
+  at += t.numel();
+  return t;
+}
+
 Tensor fresh(at::IntArrayRef shape, at::ScalarType type, const Tensor& like) {
   return at::empty(shape, like.options().dtype(type));
 }
@@ -178,10 +187,13 @@ PyObject* wb_py_route(PyObject*, PyObject* const* args, Py_ssize_t n) {
     size_t bytes = 0;
     int rc = size(ml.rows, static_cast<int32_t>(ml.cols), &bytes);
     if (rc != WB_OK) return PyLong_FromLong(rc);
-    Tensor experts = fresh({ml.rows, k}, at::kInt, logits), gates = fresh({ml.rows, k}, at::kFloat, logits);
-    Tensor positions = fresh({ml.rows, k}, at::kInt, logits), tokens = fresh({ml.rows * k}, at::kInt, logits);
-    Tensor counts = fresh({ml.cols}, at::kInt, logits), offsets = fresh({ml.cols + 1}, at::kInt, logits);
-    Tensor loss = fresh({}, at::kFloat, logits), routed = fresh({1}, at::kInt, logits);
+    // the integers in one allocation (each costs about as much as the checks)
+    const Tensor block = fresh({3 * ml.rows * k + 2 * ml.cols + 2}, at::kInt, logits);
+    int64_t next = 0;
+    Tensor experts = part(block, next, {ml.rows, k}), positions = part(block, next, {ml.rows, k});
+    Tensor tokens = part(block, next, {ml.rows * k}), counts = part(block, next, {ml.cols});
+    Tensor offsets = part(block, next, {ml.cols + 1}), routed = part(block, next, {1});
+    Tensor gates = fresh({ml.rows, k}, at::kFloat, logits), loss = fresh({}, at::kFloat, logits);
     Tensor workspace = fresh({static_cast<int64_t>(bytes)}, at::kByte, logits);
     wb_routing r{};
     r.experts = experts.data_ptr<int32_t>(), r.gates = gates.data_ptr<float>();

@@ -690,7 +690,13 @@ constexpr Choice kChoices[] = {
     {128, 128, 1, {0.655f, 0.90f}, 5.0f, {0.74f, 0.914f}, 6.0f, {}, {}},
     {256, 256, 1, {1.5f, 3.24f}, 14.5f, {1.65f, 3.31f}, 11.5f, {}, {}},
 };
+constexpr double kCodesUs = 6.0;  // the second launch, and its workspace
 constexpr int kNumChoices = sizeof(kChoices) / sizeof(kChoices[0]);
+
+// Whether a tile holds whole scales of an fp8 output.
+bool holds_scales(const LinearArgs& a, int choice) {
+  return (a.gated ? kChoices[choice].bn / 2 : kChoices[choice].bn) % kScaleBlock == 0;
+}
 
 int choose(const LinearArgs& a) {
   const int f8 = a.in_type == WB_F8E4M3;
@@ -705,17 +711,17 @@ int choose(const LinearArgs& a) {
     double tiles_m = double(row_tiles(a, c.bm));
     if (a.offsets) tiles_m = std::min(double(a.rows), double(a.rows) / c.bm + 0.5 * std::min<int64_t>(a.num_experts, a.rows));
     const double tiles = tiles_m * ((a.n_out + step - 1) / step);
-    const bool few = tiles <= 256;
-    const float per = a.direct ? (few ? c.few_us : c.us)[f8] : (few ? c.few_by_registers : c.by_registers)[f8];
-    const double us = (per * stages + (few ? c.few_fixed : c.fixed)) * (few ? 1.0 : std::ceil(tiles / (256.0 * c.resident)));
+    // a residual is read between the products and the stores, at about the
+    // stores' cost; what is left of 256 tiles or fewer has the CUs to itself
+    const int more = a.residual ? 2 : 1;
+    const double full = (a.direct ? c.us : c.by_registers)[f8] * stages + c.fixed * more;
+    const double few = (a.direct ? c.few_us : c.few_by_registers)[f8] * stages + c.few_fixed * more;
+    const double rounds = std::floor(tiles / (256 * c.resident)), left = tiles - rounds * 256 * c.resident;
+    const double us = rounds * full + (left <= 0 ? 0.0 : left <= 256 ? few : full) +
+                      (a.out_type == WB_F8E4M3 && !holds_scales(a, i) ? kCodesUs : 0.0);
     if (best < 0 || us < least) best = i, least = us;
   }
   return best;
-}
-
-// Whether a tile holds whole scales of an fp8 output.
-bool holds_scales(const LinearArgs& a, int choice) {
-  return (a.gated ? kChoices[choice].bn / 2 : kChoices[choice].bn) % kScaleBlock == 0;
 }
 
 template <class S, int CHOICE>

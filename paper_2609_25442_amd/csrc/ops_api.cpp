@@ -28,6 +28,7 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 struct Operands {
   KnownRange range;
   int rc = WB_OK;
+  bool memory = true;  // look pointers up
 
   int refuse(const std::string& msg) {
     if (rc == WB_OK) rc = set_error(WB_EINVAL, msg);
@@ -35,8 +36,7 @@ struct Operands {
   }
 
   void array(const void* p, int64_t count, int64_t bytes_each, const char* name) {
-    if (rc != WB_OK) return;
-    if (count == 0) return;
+    if (rc != WB_OK || count == 0 || !memory) return;
     rc = check_extent_as(p, count * bytes_each, [&] { return std::string(name); }, static_cast<int>(bytes_each), &range);
   }
 
@@ -51,7 +51,7 @@ struct Operands {
       refuse(std::string(name) + ": sizes or row distance out of range");
       return;
     }
-    if (rows == 0) return;
+    if (rows == 0 || !memory) return;
     const int64_t es = type_bytes(m.dtype);
     rc = check_extent_as(m.data, ((rows - 1) * m.ld + cols) * es, [&] { return std::string(name); }, static_cast<int>(es),
                          &range);
@@ -106,8 +106,10 @@ int check_route(const wb_matrix* logits, const uint8_t* mask, int32_t k, Operand
   return ops.rc;
 }
 
-// The checks of wb_linear and, after them, its launch's arguments.
-int check_linear(const wb_linear_args* p, Operands& ops, wb::LinearArgs& a) {
+// The checks of wb_linear and, after them, its launch's arguments. Without
+// `memory`, for the workspace's size, pointers are not looked up.
+int check_linear(const wb_linear_args* p, Operands& ops, wb::LinearArgs& a, bool memory) {
+  ops.memory = memory;
   if (!p) return set_error(WB_EINVAL, "null argument");
   const bool stacked = p->num_experts > 0;
   if (p->num_experts < 0 || p->num_experts > 65536) return set_error(WB_EINVAL, "num_experts outside 0..65536");
@@ -287,7 +289,7 @@ int wb_linear_workspace(const wb_linear_args* p, size_t* bytes) {
     if (!bytes) return set_error(WB_EINVAL, "null argument");
     Operands ops;
     wb::LinearArgs a{};
-    const int rc = check_linear(p, ops, a);
+    const int rc = check_linear(p, ops, a, false);
     if (rc != WB_OK) return rc;
     *bytes = wb::linear_workspace_bytes(a);
     return WB_OK;
@@ -298,7 +300,7 @@ int wb_linear(const wb_linear_args* p, void* workspace, size_t workspace_bytes, 
   return guarded([&]() -> int {
     Operands ops;
     wb::LinearArgs a{};
-    const int rc = check_linear(p, ops, a);
+    const int rc = check_linear(p, ops, a, true);
     if (rc != WB_OK) return rc;
     const size_t need = wb::linear_workspace_bytes(a);
     if (workspace_bytes < need) return set_error(WB_ESIZE, "workspace smaller than wb_linear_workspace");
