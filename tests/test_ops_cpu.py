@@ -1,0 +1,115 @@
+"""What the operators' C entries refuse before they look at memory, and the
+sizes they ask for, without a GPU."""
+
+import ctypes
+
+import pytest
+
+import paper_2609_25442_amd as wb
+
+F32, BF16, F8 = 0, 1, 2
+
+
+class Matrix(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("ld", ctypes.c_int64)]
+
+
+class Args(ctypes.Structure):
+    _fields_ = [(f, Matrix) for f in ("x", "x_scales", "weight", "weight_scales", "bias", "residual", "out", "out_scales")]
+    _fields_ += [("offsets", ctypes.c_void_p), ("tokens", ctypes.c_void_p), ("num_experts", ctypes.c_int32),
+                 ("activation", ctypes.c_int32), ("gated", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+def m(rows, cols, dtype=BF16, ld=None, data=4096):
+    return Matrix(data, dtype, 0, rows, cols, cols if ld is None else ld)
+
+
+def linear(**more):
+    a = Args()
+    a.x, a.weight, a.out = m(4, 64), m(32, 64), m(4, 32)
+    for k, v in more.items():
+        setattr(a, k, v)
+    return a
+
+
+def workspace(a):
+    n = ctypes.c_size_t(0)
+    return wb.lib.wb_linear_workspace(ctypes.byref(a), ctypes.byref(n)), n.value
+
+
+def test_linear_workspace_of_plain_results_is_none():
+    assert workspace(linear()) == (wb.WB_OK, 0)
+    assert workspace(linear(out=m(4, 32, F32))) == (wb.WB_OK, 0)
+    assert workspace(linear(x=m(0, 64), out=m(0, 32))) == (wb.WB_OK, 0)
+
+
+def test_linear_workspace_of_fp8_results_holds_fp32_rows():
+    a = linear(weight=m(4096, 64), out=m(4, 4096, F8), out_scales=m(4, 32, F32))
+    rc, n = workspace(a)
+    assert rc == wb.WB_OK and n in (0, 4 * 4096 * 4)
+
+
+@pytest.mark.parametrize("more,code", [
+    (dict(x=m(4, 63)), wb.WB_EINVAL), (dict(out=m(4, 31)), wb.WB_EINVAL), (dict(out=m(3, 32)), wb.WB_EINVAL),
+    (dict(x=m(4, 64, ld=63)), wb.WB_EINVAL), (dict(gated=1), wb.WB_EINVAL), (dict(activation=3), wb.WB_EINVAL),
+    (dict(x=m(4, 64, F32)), wb.WB_EUNSUPPORTED), (dict(x=m(4, 64, F8)), wb.WB_EUNSUPPORTED),
+    (dict(x=m(4, 64, F8), weight=m(32, 64, F8)), wb.WB_EINVAL),
+    (dict(x=m(4, 64, F8), weight=m(32, 64, F8), x_scales=m(4, 1, F32), weight_scales=m(2, 1, F32)), wb.WB_EINVAL),
+    (dict(x_scales=m(4, 1, F32)), wb.WB_EINVAL), (dict(bias=m(1, 31, F32)), wb.WB_EINVAL),
+    (dict(bias=m(1, 32, F8)), wb.WB_EINVAL), (dict(residual=m(4, 31)), wb.WB_EINVAL),
+    (dict(out=m(4, 32, F8)), wb.WB_EINVAL), (dict(out_scales=m(4, 1, F32)), wb.WB_EINVAL),
+    (dict(out=m(4, 32, F8), out_scales=m(4, 2, F32)), wb.WB_EINVAL), (dict(offsets=4096), wb.WB_EINVAL),
+    (dict(tokens=4096), wb.WB_EINVAL), (dict(num_experts=2), wb.WB_EINVAL), (dict(num_experts=-1), wb.WB_EINVAL),
+    (dict(num_experts=3, offsets=4096), wb.WB_EINVAL), (dict(x=m(1 << 22, 64), out=m(1 << 22, 32)), wb.WB_EUNSUPPORTED),
+    (dict(x=m(-1, 64)), wb.WB_EINVAL), (dict(x=m(4, 0), weight=m(32, 0)), wb.WB_EINVAL),
+])
+def test_linear_refuses(more, code):
+    a = linear(**more)
+    assert workspace(a)[0] == code
+    assert wb.lib.wb_last_error()
+    assert wb.lib.wb_linear(ctypes.byref(a), None, ctypes.c_size_t(0), None) == code
+
+
+def test_linear_refuses_memory_the_gpu_cannot_address():
+    buf = ctypes.create_string_buffer(1 << 16)
+    at = (ctypes.addressof(buf) + 255) // 256 * 256
+    a = linear(x=m(4, 64, data=at), weight=m(32, 64, data=at + 8192), out=m(4, 32, data=at + 16384))
+    assert wb.lib.wb_linear(ctypes.byref(a), None, ctypes.c_size_t(0), None) == wb.WB_EINVAL
+
+
+def test_null_arguments_are_refused():
+    f, z = wb.lib, ctypes.c_size_t(0)
+    assert f.wb_linear(None, None, z, None) == wb.WB_EINVAL
+    assert f.wb_linear_workspace(None, ctypes.byref(z)) == wb.WB_EINVAL
+    assert f.wb_linear_workspace(ctypes.byref(linear()), None) == wb.WB_EINVAL
+    assert f.wb_route(None, None, 1, 0, None, None, z, None) == wb.WB_EINVAL
+    assert f.wb_route_backward(None, None, 1, 0, None, None, None, None, None) == wb.WB_EINVAL
+    assert f.wb_add_rms_norm(None, None, None, ctypes.c_float(0), None, None, None, None) == wb.WB_EINVAL
+    assert f.wb_combine(None, None, None, 1, None, None, None, None, None) == wb.WB_EINVAL
+    assert f.wb_route_workspace(ctypes.c_int64(4), 8, None) == wb.WB_EINVAL
+
+
+@pytest.mark.parametrize("rows,experts,code", [(0, 1, 0), (1, 8, 0), (64, 1024, 0), (65, 256, 0), (4194303, 8, 0),
+                                               (-1, 8, wb.WB_EINVAL), (4, 0, wb.WB_EINVAL), (4, 1025, wb.WB_EUNSUPPORTED),
+                                               (4194304, 8, wb.WB_EUNSUPPORTED)])
+def test_route_workspace(rows, experts, code):
+    n = ctypes.c_size_t(0)
+    assert wb.lib.wb_route_workspace(ctypes.c_int64(rows), experts, ctypes.byref(n)) == code
+    if code == 0:
+        # one sum and one count per expert, and the rows sent, for at most 256 blocks of rows
+        assert 8 * experts + 4 <= n.value <= 256 * (8 * experts + 4)
+
+
+def test_operators_refuse_cpu_tensors():
+    import torch
+
+    if torch.cuda.is_available():
+        pytest.skip("the GPU's own refusals are tested there")
+    x = torch.zeros(2, 8)
+    with pytest.raises(wb.WbError):
+        wb.add_rms_norm(x, x[0], out_dtype="f16")
+    with pytest.raises(wb.WbError):
+        wb.linear(x, x, activation="tanh")
+    with pytest.raises(wb.WbError):
+        wb.expert_linear(x, x, None)
