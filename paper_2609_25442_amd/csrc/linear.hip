@@ -10,6 +10,7 @@
 // fp8 codes are widened to bf16 (exactly) on their way to the matrix cores;
 // the sums of a block are scaled and added in fp32.
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <type_traits>
 
@@ -21,7 +22,6 @@ namespace {
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef u32x4 u32x4_a1 __attribute__((aligned(1)));
-typedef u32x2 u32x2_a2 __attribute__((aligned(2)));
 typedef uint32_t u32_a1 __attribute__((aligned(1)));
 
 constexpr int kStageBytes = 128;  // of a row, per step over k: a scale block of fp8, half as many bf16
@@ -124,14 +124,7 @@ __device__ __forceinline__ u32x4 load_piece(const uint8_t* row, int64_t at, int6
 // Four neighbouring columns of a row; in: how many of them exist.
 __device__ __forceinline__ void load_four(const void* base, int64_t at, int type, int in, float (&v)[4]) {
   if (in >= 4) {
-    if (type == WB_F32) {
-      const f32x4 f = *reinterpret_cast<const f32x4_a4*>(static_cast<const float*>(base) + at);
-      for (int r = 0; r < 4; ++r) v[r] = f[r];
-    } else {
-      const u32x2 u = *reinterpret_cast<const u32x2_a2*>(static_cast<const uint16_t*>(base) + at);
-      for (int r = 0; r < 4; ++r)
-        v[r] = __builtin_bit_cast(float, (r & 1) ? u[r >> 1] & 0xffff0000u : u[r >> 1] << 16);
-    }
+    wb::load_four(base, at, type, v);
   } else {
     for (int r = 0; r < 4; ++r) v[r] = r < in ? load_one(base, at + r, type) : 0.0f;
   }
@@ -146,10 +139,7 @@ __device__ __forceinline__ void store_four(void* base, int64_t at, int type, int
     else
       for (int r = 0; r < in; ++r) to[r] = static_cast<uint8_t>(p >> (8 * r));
   } else if (in >= 4) {
-    if (type == WB_F32)
-      *reinterpret_cast<f32x4_a4*>(static_cast<float*>(base) + at) = f32x4{v[0], v[1], v[2], v[3]};
-    else
-      *reinterpret_cast<u32x2_a2*>(static_cast<uint16_t*>(base) + at) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+    wb::store_four(base, at, type, v);
   } else {
     for (int r = 0; r < in; ++r) store_one(base, at + r, type, v[r]);
   }
@@ -651,8 +641,17 @@ int64_t row_tiles(const LinearArgs& a, int per) {
 template <class S, bool F8, bool DIRECT>
 hipError_t launch_tile(const LinearArgs& a, hipStream_t st) {
   const auto kernel = wb_linear_tile_kernel<S, F8, DIRECT>;
-  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds);
+  // the kernel's LDS is past the default limit; once for each GPU of a process
+  static std::atomic<uint64_t> raised{0};
+  int device = 0;
+  hipError_t e = hipGetDevice(&device);
   if (e != hipSuccess) return e;
+  const uint64_t bit = device < 64 ? uint64_t(1) << device : 0;
+  if (!(raised.load(std::memory_order_acquire) & bit) || !bit) {
+    e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds);
+    if (e != hipSuccess) return e;
+    raised.fetch_or(bit, std::memory_order_release);
+  }
   const int step = a.gated ? S::BN / 2 : S::BN;
   const int64_t tiles_n = (a.n_out + step - 1) / step;
   const int64_t all = row_tiles(a, S::BM) * tiles_n;

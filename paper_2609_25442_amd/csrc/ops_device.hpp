@@ -129,6 +129,26 @@ __device__ __forceinline__ void store_tail(void* row, int64_t col, int64_t cols,
     if (col + i < cols) store_one(row, col + i, type, v[i]);
 }
 
+// Four neighbouring columns.
+typedef u32x2 u32x2_a2 __attribute__((aligned(2)));
+
+__device__ __forceinline__ void load_four(const void* row, int64_t col, int type, float (&v)[4]) {
+  if (type == WB_F32) {
+    const f32x4 f = *reinterpret_cast<const f32x4_a4*>(static_cast<const float*>(row) + col);
+    for (int r = 0; r < 4; ++r) v[r] = f[r];
+  } else {
+    const u32x2 u = *reinterpret_cast<const u32x2_a2*>(static_cast<const uint16_t*>(row) + col);
+    for (int r = 0; r < 4; ++r) v[r] = __builtin_bit_cast(float, (r & 1) ? u[r >> 1] & 0xffff0000u : u[r >> 1] << 16);
+  }
+}
+
+__device__ __forceinline__ void store_four(void* row, int64_t col, int type, const float (&v)[4]) {
+  if (type == WB_F32)
+    *reinterpret_cast<f32x4_a4*>(static_cast<float*>(row) + col) = f32x4{v[0], v[1], v[2], v[3]};
+  else
+    *reinterpret_cast<u32x2_a2*>(static_cast<uint16_t*>(row) + col) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+}
+
 // The sixteen lanes of a row, turned by N: every lane gets the result of a
 // reduction after N = 8, 4, 2, 1, in vector instructions alone.
 template <int N, class T>

@@ -10,10 +10,12 @@
 //           chosen instead
 //   out_t = residual_t + sum_i gates_ti y[positions_ti]
 //
-// Bandwidth bound on paper, by latency in fact: a row's logits are a few
-// hundred bytes. Sixteen lanes hold a row (four rows to a wavefront), so every
-// reduction is four steps inside a row of lanes, and choosing an expert costs
-// two passes over E / 16 registers.
+// The bytes are few; choosing is what takes time, k times a row's largest and
+// its place. Eight lanes hold a row (sixteen past 256 experts), so that the
+// steps of a reduction serve eight rows at once. Measured with 32768 x 256
+// fp32 logits, k = 8: choices 23 us (27 with a pass over every lane's registers
+// for each choice, 29 with sixteen lanes a row), places 14.5, gradient 19 (the
+// 67 MB that it moves take 10); 35 us the forward calls, 53 with the gradient.
 //
 // Places in expert order need every row's choice first: two launches, the
 // first over blocks of rows (choices, gates, and per block the counts and the
@@ -29,12 +31,41 @@
 namespace wb {
 namespace {
 
+// A lane's neighbour within eight.
+template <int CTRL, class V>
+__device__ __forceinline__ V lanes8(V v) {
+  const int i = __builtin_bit_cast(int, v);
+  return __builtin_bit_cast(V, __builtin_amdgcn_update_dpp(i, i, CTRL, 0xf, 0xf, false));
+}
+
 constexpr int kOneBlockRows = 64;  // up to here one launch
 constexpr int kMaxBlocks = 256;    // blocks of rows: one per CU
-constexpr int kGradThreads = 256, kGradBlocks = 1024;
+constexpr int kGradThreads = 256, kGradBlocks = 1024, kPlaceThreads = 1024;
 
-// Threads of a workgroup whose lanes hold R logits: as many as the registers allow.
-constexpr int route_threads(int r) { return r <= 16 ? 1024 : r <= 32 ? 512 : 256; }
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+typedef i32x4 i32x4_a4 __attribute__((aligned(4)));
+
+// Rows lie over L lanes with R registers each: lane l holds experts 4 l, ...,
+// 4 l + 3 of every 4 L, or l of every L where R is 1. T: threads of a
+// workgroup, as many as the registers allow.
+template <int L_, int R_>
+struct Row {
+  static constexpr int L = L_, R = R_, E = L * R, T = R <= 8 ? 1024 : R <= 32 ? 512 : 256;
+  __device__ static int expert(int l, int j) { return R == 1 ? l : (j >> 2) * (4 * L) + 4 * l + (j & 3); }
+  // and back
+  __device__ static int lane(int e) { return R == 1 ? e % L : e / 4 % L; }
+  __device__ static int place(int e) { return R == 1 ? 0 : e / (4 * L) % (R / 4 > 0 ? R / 4 : 1) * 4 + e % 4; }
+  template <class V, class Op>
+  __device__ __forceinline__ static V reduce(V v, Op op) {
+    if constexpr (L == 16) {
+      return reduce16(v, op);
+    } else {
+      v = op(v, lanes8<0xB1>(v));    // pairs
+      v = op(v, lanes8<0x4E>(v));    // fours
+      return op(v, lanes8<0x141>(v));  // eights, mirrored
+    }
+  }
+};
 
 int64_t rows_per_block(int64_t rows) {
   if (rows <= kOneBlockRows) return kOneBlockRows;
@@ -57,104 +88,159 @@ __host__ __device__ Partials partials(void* workspace, int64_t blocks, int32_t e
   return p;
 }
 
-// The logits of a row: lane l of the sixteen holds experts l, l + 16, ...
-template <int R>
+template <class W>
 __device__ __forceinline__ void load_logits(const void* base, int64_t row, int64_t ld, int type, int experts, int l,
-                                            float (&z)[R]) {
+                                            float (&z)[W::R]) {
   const char* at = static_cast<const char*>(base) + row * ld * (type == WB_F32 ? 4 : 2);
+  if constexpr (W::R == 1) {
+    z[0] = l < experts ? load_one(at, l, type) : -__builtin_inff();
+  } else {
 #pragma unroll
-  for (int j = 0; j < R; ++j) z[j] = l + 16 * j < experts ? load_one(at, l + 16 * j, type) : -__builtin_inff();
+    for (int j = 0; j < W::R; j += 4) {
+      const int e = W::expert(l, j);
+      float v[4];
+      if (e + 4 <= experts) {
+        load_four(at, e, type, v);
+      } else {
+        for (int i = 0; i < 4; ++i) v[i] = e + i < experts ? load_one(at, e + i, type) : -__builtin_inff();
+      }
+      for (int i = 0; i < 4; ++i) z[j + i] = v[i];
+    }
+  }
 }
 
-// exp(z - top) of a row, its largest logit and one over the sum, and whether
-// the row has a logit above -inf. A NaN or +inf logit makes the sum NaN.
-template <int R>
-__device__ __forceinline__ bool softmax_row(const float (&z)[R], float (&e)[R], float& r) {
-  float top = -__builtin_inff();
+// exp(x) of x <= 0, to within two roundings: 2^(x log2 e), the product's
+// remainder and the constant's put back in.
+__device__ __forceinline__ float exp_below(float x) {
+  x = x < -150.0f ? -150.0f : x;  // 0; NaN stays
+  const float hi = x * 1.44269502f, lo = __builtin_fmaf(x, 1.92596299e-8f, __builtin_fmaf(x, 1.44269502f, -hi));
+  const float e = __builtin_amdgcn_exp2f(hi);
+  return __builtin_fmaf(e * lo, 0.693147182f, e);
+}
+
+// exp(z - top) of a row, one over the sum, and whether the row has a logit
+// above -inf. A NaN or +inf logit makes the sum NaN.
+template <class W>
+__device__ __forceinline__ bool softmax_row(const float (&z)[W::R], float (&e)[W::R], float& r, float& top) {
+  top = -__builtin_inff();
 #pragma unroll
-  for (int j = 0; j < R; ++j) top = fmaxf(top, z[j]);
-  top = reduce16(top, FMax());
+  for (int j = 0; j < W::R; ++j) top = fmaxf(top, z[j]);
+  top = W::reduce(top, FMax());
+  if (top == -__builtin_inff()) top = 0.0f;
   float sum = 0.0f;
 #pragma unroll
-  for (int j = 0; j < R; ++j) {
-    e[j] = z[j] == -__builtin_inff() ? 0.0f : expf(z[j] - top);
+  for (int j = 0; j < W::R; ++j) {
+    e[j] = exp_below(z[j] - top);
     sum += e[j];
   }
-  sum = reduce16(sum, Sum());
+  sum = W::reduce(sum, Sum());
   r = 1.0f / sum;
   return sum != 0.0f;
 }
 
 // Choices, gates and partial sums of one block of rows.
-template <int R>
+template <class W>
 __device__ void route_block(const RouteArgs& a, const Partials& part, int64_t block, int64_t per) {
-  constexpr int T = route_threads(R);
-  __shared__ float s_sum[T / 64][16 * R];
-  __shared__ int32_t s_count[16 * R];
+  constexpr int T = W::T, R = W::R, L = W::L;
+  __shared__ float s_sum[T / 64][W::E];
+  __shared__ int32_t s_count[W::E];
   __shared__ int32_t s_routed;
-  const int l = threadIdx.x & 15, group = threadIdx.x >> 4;
-  for (int e = threadIdx.x; e < 16 * R; e += T) s_count[e] = 0;
+  constexpr bool kShared = R >= 2 * L;
+  constexpr int kPitch = R + 1;  // of a lane's logits
+  __shared__ float s_row[kShared ? T / L * L * kPitch : 1];
+  __shared__ float s_gate[T / L][kMaxRouteK + 1];  // a row's, until their sum is known
+  __shared__ int32_t s_expert[T / L][kMaxRouteK + 1];
+  const int l = threadIdx.x % L, group = threadIdx.x / L;
+  for (int e = threadIdx.x; e < W::E; e += T) s_count[e] = 0;
   if (threadIdx.x == 0) s_routed = 0;
   __syncthreads();
   float acc[R];
 #pragma unroll
   for (int j = 0; j < R; ++j) acc[j] = 0.0f;
   const int64_t end = min(a.rows, (block + 1) * per);
-  for (int64_t row = block * per + group; row < end; row += T / 16) {
-    float z[R], e[R], r;
-    load_logits<R>(a.logits, row, a.ld_logits, a.logits_type, a.num_experts, l, z);
-    bool routed = softmax_row<R>(z, e, r);
-    if (a.mask && !a.mask[row]) routed = false;
+  for (int64_t row = block * per + group; row < end; row += T / L) {
+    float z[R], e[R], r, top;
+    const bool masked = a.mask && !a.mask[row];
+    load_logits<W>(a.logits, row, a.ld_logits, a.logits_type, a.num_experts, l, z);
+    const bool routed = softmax_row<W>(z, e, r, top) && !masked;
     if (routed) {
 #pragma unroll
       for (int j = 0; j < R; ++j) acc[j] = __builtin_fmaf(e[j], r, acc[j]);
       if (l == 0) atomicAdd(&s_routed, 1);
     }
-    // lane i % 16 keeps choice i and writes it with its fifteen neighbours'
-    float chosen = 0.0f, gate = 0.0f;
-    int expert = -1;
+    // Every lane knows its largest; a choice asks for the row's, and only the
+    // lane that had it needs its next, which all the lanes of the row look for
+    // in the row's copy in LDS: a third of the instructions of a pass over
+    // every lane's registers, where those are many.
+    float lane_best = -__builtin_inff(), chosen = 0.0f;
+    int lane_at = W::E;
+    float* const mine = s_row + group * (L * kPitch);
+    if constexpr (kShared) {
+      order_lanes();
+#pragma unroll
+      for (int j = 0; j < R; ++j) lane_best = fmaxf(lane_best, z[j]), mine[l * kPitch + j] = z[j];
+#pragma unroll
+      for (int j = R - 1; j >= 0; --j) lane_at = z[j] == lane_best ? W::expert(l, j) : lane_at;
+    }
     for (int i = 0; i < a.k; ++i) {
-      float best = -__builtin_inff();
+      float best;
+      int at;
+      if constexpr (kShared) {
+        best = W::reduce(lane_best, FMax());
+        at = W::reduce(lane_best == best ? lane_at : W::E, IMin());
+        // its lane's next, looked for by all the lanes of the row
+        const int from = W::lane(at), here = l * (R / L);
+        order_lanes();
+        if (l == 0) mine[from * kPitch + W::place(at)] = -__builtin_inff();
+        order_lanes();
+        float v[R / L], most = -__builtin_inff();
 #pragma unroll
-      for (int j = 0; j < R; ++j) best = fmaxf(best, z[j]);
-      best = reduce16(best, FMax());
-      int at = 16 * R;
+        for (int j = 0; j < R / L; ++j) v[j] = mine[from * kPitch + here + j], most = fmaxf(most, v[j]);
+        most = W::reduce(most, FMax());
+        int next = R;
 #pragma unroll
-      for (int j = R - 1; j >= 0; --j) at = z[j] == best ? l + 16 * j : at;
-      at = reduce16(at, IMin());
-      float g = 0.0f;
+        for (int j = R / L - 1; j >= 0; --j) next = v[j] == most ? here + j : next;
+        next = W::reduce(next, IMin());
+        if (l == from) lane_best = most, lane_at = W::expert(l, next < R ? next : 0);
+      } else {
+        best = -__builtin_inff();
 #pragma unroll
-      for (int j = 0; j < R; ++j)
-        if (at == l + 16 * j) g = e[j], z[j] = -__builtin_inff();
-      g = __shfl(g, at & 15, 16);  // from the lane that holds it
+        for (int j = 0; j < R; ++j) best = fmaxf(best, z[j]);
+        best = W::reduce(best, FMax());
+        at = W::E;
+#pragma unroll
+        for (int j = R - 1; j >= 0; --j) at = z[j] == best ? W::expert(l, j) : at;
+        at = W::reduce(at, IMin());
+#pragma unroll
+        for (int j = 0; j < R; ++j) z[j] = at == W::expert(l, j) ? -__builtin_inff() : z[j];
+      }
+      float g = exp_below(best - top) + (r - r);  // NaN where the row's sum is
       const bool none = !routed || best == -__builtin_inff();
       if (none) at = -1, g = 0.0f;
-      if (!none && l == 0) atomicAdd(&s_count[at], 1);
       chosen += g;
-      if (l == (i & 15)) expert = at, gate = g * r;
-      if ((i & 15) == 15 || i == a.k - 1) {
-        const int first = i & ~15;
-        if (l <= i - first) {
-          a.experts[row * a.k + first + l] = expert;
-          a.gates[row * a.k + first + l] = expert < 0 ? 0.0f : gate;
-        }
+      if (l == 0) {
+        s_gate[group][i] = g;
+        s_expert[group][i] = at;
+        if (!none) atomicAdd(&s_count[at], 1);
       }
     }
-    if (a.renormalize && routed) {
-      // over the sum of the chosen instead: r is 1 / the sum of all, so the
-      // quotient of both is what the gates are still to be multiplied by
-      const float more = 1.0f / (chosen * r);
-      for (int i = l; i < a.k; i += 16)
-        if (a.experts[row * a.k + i] >= 0) a.gates[row * a.k + i] *= more;
+    // over the sum of the chosen, or of all
+    const float scale = a.renormalize ? 1.0f / chosen : r;
+    order_lanes();
+    for (int i = l; i < a.k; i += L) {
+      const int at = s_expert[group][i];
+      a.experts[row * a.k + i] = at;
+      a.gates[row * a.k + i] = at < 0 ? 0.0f : s_gate[group][i] * scale;
     }
+    order_lanes();
   }
-  // four rows of a wavefront, then the wavefronts in order
+  // the rows of a wavefront, then the wavefronts in order
   const int wave = threadIdx.x >> 6;
 #pragma unroll
   for (int j = 0; j < R; ++j) {
-    acc[j] += __shfl_xor(acc[j], 16);
-    acc[j] += __shfl_xor(acc[j], 32);
-    if ((threadIdx.x & 63) < 16) s_sum[wave][l + 16 * j] = acc[j];
+#pragma unroll
+    for (int off = L; off < 64; off <<= 1) acc[j] += __shfl_xor(acc[j], off);
+    if ((threadIdx.x & 63) < L) s_sum[wave][W::expert(l, j)] = acc[j];
   }
   __syncthreads();
   for (int e = threadIdx.x; e < a.num_experts; e += T) {
@@ -167,27 +253,35 @@ __device__ void route_block(const RouteArgs& a, const Partials& part, int64_t bl
 }
 
 // Places of one block of rows; block == blocks: totals and loss.
-template <int R>
+template <class W, int T>
 __device__ void place_block(const RouteArgs& a, const Partials& part, int64_t block, int64_t blocks, int64_t per) {
-  constexpr int E = 16 * R, T = route_threads(R), G = T / E > 0 ? T / E : 1, kRows = 64, kWords = kRows / 32;
+  constexpr int E = W::E, Q = E / 4, G = T / Q < 16 ? T / Q : 16, kRows = 64, kWords = kRows / 32;
+  static_assert(G >= 1, "a thread for every four experts");
   __shared__ int32_t s_part[G][E], s_before[G][E], s_total[E], s_base[E], s_wave[T / 64];
   __shared__ uint32_t s_bits[E][kWords];
   __shared__ float s_loss[T / 64];
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   // counts over all blocks, and over those before this one: G sets of threads
-  // take every G-th block
-  for (int e = t % E; e < E; e += T) {
-    int32_t total = 0, before = 0;
-    if (e < a.num_experts) {
-#pragma unroll 16
-      for (int64_t b = t / E; b < blocks; b += G) {
-        const int32_t c = part.counts[b * a.num_experts + e];
+  // take every G-th block, a thread four experts
+  if (t < Q * G) {
+    const int e = t % Q * 4, in = a.num_experts - e;
+    i32x4 total = {0, 0, 0, 0}, before = {0, 0, 0, 0};
+    if (in >= 4) {
+#pragma unroll 8
+      for (int64_t b = t / Q; b < blocks; b += G) {
+        const i32x4 c = *reinterpret_cast<const i32x4_a4*>(part.counts + b * a.num_experts + e);
         total += c;
-        before += b < block ? c : 0;
+        before += b < block ? c : i32x4{0, 0, 0, 0};
       }
+    } else {
+      for (int64_t b = t / Q; b < blocks; b += G)
+        for (int i = 0; i < 4; ++i) {
+          const int32_t c = i < in ? part.counts[b * a.num_experts + e + i] : 0;
+          total[i] += c;
+          before[i] += b < block ? c : 0;
+        }
     }
-    s_part[t / E % G][e] = total;
-    s_before[t / E % G][e] = before;
+    for (int i = 0; i < 4; ++i) s_part[t / Q][e + i] = total[i], s_before[t / Q][e + i] = before[i];
   }
   __syncthreads();
   // exclusive prefix of the totals, T experts at a time
@@ -218,11 +312,20 @@ __device__ void place_block(const RouteArgs& a, const Partials& part, int64_t bl
   }
   if (block == blocks) {
     float loss = 0.0f;
-    for (int e = t % E; e < a.num_experts; e += T) {
-      float s = 0.0f;
-#pragma unroll 16
-      for (int64_t b = t / E; b < blocks; b += G) s += part.sums[b * a.num_experts + e];
-      loss = __builtin_fmaf(s, static_cast<float>(s_total[e]), loss);
+    if (t < Q * G) {
+      const int e = t % Q * 4, in = min(4, a.num_experts - e);
+      float sum[4] = {0, 0, 0, 0};
+      if (in == 4) {
+#pragma unroll 8
+        for (int64_t b = t / Q; b < blocks; b += G) {
+          const f32x4 p = *reinterpret_cast<const f32x4_a4*>(part.sums + b * a.num_experts + e);
+          for (int i = 0; i < 4; ++i) sum[i] += p[i];
+        }
+      } else {
+        for (int64_t b = t / Q; b < blocks; b += G)
+          for (int i = 0; i < in; ++i) sum[i] += part.sums[b * a.num_experts + e + i];
+      }
+      for (int i = 0; i < in; ++i) loss = __builtin_fmaf(sum[i], static_cast<float>(s_total[e + i]), loss);
     }
     int32_t n = 0;
     for (int64_t b = t; b < blocks; b += T) n += part.routed[b];
@@ -274,41 +377,41 @@ __device__ void place_block(const RouteArgs& a, const Partials& part, int64_t bl
   }
 }
 
-template <int R>
-__global__ __launch_bounds__(route_threads(R)) void wb_route_kernel(RouteArgs a, int64_t blocks, int64_t per) {
-  route_block<R>(a, partials(a.workspace, blocks, a.num_experts), blockIdx.x, per);
+template <class W>
+__global__ __launch_bounds__(W::T) void wb_route_kernel(RouteArgs a, int64_t blocks, int64_t per) {
+  route_block<W>(a, partials(a.workspace, blocks, a.num_experts), blockIdx.x, per);
 }
 
-template <int R>
-__global__ __launch_bounds__(route_threads(R)) void wb_route_place_kernel(RouteArgs a, int64_t blocks, int64_t per) {
-  place_block<R>(a, partials(a.workspace, blocks, a.num_experts), blockIdx.x, blocks, per);
+template <class W>
+__global__ __launch_bounds__(kPlaceThreads) void wb_route_place_kernel(RouteArgs a, int64_t blocks, int64_t per) {
+  place_block<W, kPlaceThreads>(a, partials(a.workspace, blocks, a.num_experts), blockIdx.x, blocks, per);
 }
 
 // All of it for the rows of one block.
-template <int R>
-__global__ __launch_bounds__(route_threads(R)) void wb_route_few_kernel(RouteArgs a, int64_t per) {
+template <class W>
+__global__ __launch_bounds__(W::T) void wb_route_few_kernel(RouteArgs a, int64_t per) {
   const Partials part = partials(a.workspace, 1, a.num_experts);
   if (a.rows) {
-    route_block<R>(a, part, 0, per);
+    route_block<W>(a, part, 0, per);
   } else {
-    for (int e = threadIdx.x; e < a.num_experts; e += route_threads(R)) part.sums[e] = 0.0f, part.counts[e] = 0;
+    for (int e = threadIdx.x; e < a.num_experts; e += W::T) part.sums[e] = 0.0f, part.counts[e] = 0;
     if (threadIdx.x == 0) part.routed[0] = 0;
   }
   __threadfence_block();
   __syncthreads();
-  place_block<R>(a, part, 0, 1, per);
+  place_block<W, W::T>(a, part, 0, 1, per);
   __syncthreads();
-  place_block<R>(a, part, 1, 1, per);
+  place_block<W, W::T>(a, part, 1, 1, per);
 }
 
-// Sixteen lanes a row. What the gates add at a row's choices goes through the
+// What the gates add at a row's choices goes through the
 // row's copy in LDS, lane i adding choice i's (the choices are different
-// experts): k times E / 16 selections between registers take longer.
-template <int R>
+// experts): k times R selections between registers take longer.
+template <class W>
 __global__ __launch_bounds__(kGradThreads) void wb_route_grad_kernel(RouteGradArgs a) {
-  constexpr int E = 16 * R, kGroups = kGradThreads / 16, kPitch = E + 1;
+  constexpr int R = W::R, L = W::L, kGroups = kGradThreads / L, kPitch = W::E + 1;
   __shared__ float s_row[kGroups * kPitch];
-  const int l = threadIdx.x & 15, group = threadIdx.x >> 4;
+  const int l = threadIdx.x % L, group = threadIdx.x / L;
   float* const mine = s_row + group * kPitch;
   const float n = static_cast<float>(*a.routed);
   const float scale = a.d_loss && n > 0.0f
@@ -317,12 +420,19 @@ __global__ __launch_bounds__(kGradThreads) void wb_route_grad_kernel(RouteGradAr
   float of_loss[R];
 #pragma unroll
   for (int j = 0; j < R; ++j)
-    of_loss[j] = l + 16 * j < a.num_experts ? scale * static_cast<float>(a.counts[l + 16 * j]) : 0.0f;
+    of_loss[j] = W::expert(l, j) < a.num_experts ? scale * static_cast<float>(a.counts[W::expert(l, j)]) : 0.0f;
   const int64_t stride = int64_t(gridDim.x) * kGroups;
   for (int64_t row = int64_t(blockIdx.x) * kGroups + group; row < a.rows; row += stride) {
-    float z[R], p[R], d[R], r;
-    load_logits<R>(a.logits, row, a.ld_logits, a.logits_type, a.num_experts, l, z);
-    const bool routed = softmax_row<R>(z, p, r) && (!a.mask || a.mask[row]);
+    float z[R], p[R], d[R], r, top;
+    // the lane's first choice, on its way with the logits
+    struct {
+      int32_t expert;
+      float gate, d;
+    } first = {-1, 0.0f, 0.0f};
+    if (a.d_gates && l < a.k) first = {a.experts[row * a.k + l], a.gates[row * a.k + l], a.d_gates[row * a.k + l]};
+    const bool masked = a.mask && !a.mask[row];
+    load_logits<W>(a.logits, row, a.ld_logits, a.logits_type, a.num_experts, l, z);
+    const bool routed = softmax_row<W>(z, p, r, top) && !masked;
     const int32_t* experts = a.experts + row * a.k;
     const float* gates = a.gates + row * a.k;
     const float* d_gates = a.d_gates ? a.d_gates + row * a.k : nullptr;
@@ -330,41 +440,52 @@ __global__ __launch_bounds__(kGradThreads) void wb_route_grad_kernel(RouteGradAr
     for (int j = 0; j < R; ++j) p[j] *= r, d[j] = of_loss[j];
     if (d_gates && !a.renormalize) {
 #pragma unroll
-      for (int j = 0; j < R; ++j) mine[l + 16 * j] = d[j];
+      for (int j = 0; j < R; ++j) mine[W::expert(l, j)] = d[j];
       order_lanes();
-      for (int i = l; i < a.k; i += 16) {
-        const int e = experts[i];
-        if (e >= 0) mine[e] += d_gates[i];
-      }
+      if (first.expert >= 0) mine[first.expert] += first.d;
+      for (int i = l + L; i < a.k; i += L)
+        if (experts[i] >= 0) mine[experts[i]] += d_gates[i];
       order_lanes();
 #pragma unroll
-      for (int j = 0; j < R; ++j) d[j] = mine[l + 16 * j];
+      for (int j = 0; j < R; ++j) d[j] = mine[W::expert(l, j)];
     }
     float mean = 0.0f;
 #pragma unroll
     for (int j = 0; j < R; ++j) mean = __builtin_fmaf(p[j], d[j], mean);
-    mean = reduce16(mean, Sum());
+    mean = W::reduce(mean, Sum());
 #pragma unroll
     for (int j = 0; j < R; ++j) d[j] = p[j] * (d[j] - mean);
     if (d_gates && a.renormalize) {
 #pragma unroll
-      for (int j = 0; j < R; ++j) mine[l + 16 * j] = d[j];
-      float dot = 0.0f;
-      for (int i = l; i < a.k; i += 16) dot += experts[i] >= 0 ? gates[i] * d_gates[i] : 0.0f;
-      dot = reduce16(dot, Sum());
+      for (int j = 0; j < R; ++j) mine[W::expert(l, j)] = d[j];
+      float dot = first.expert >= 0 ? first.gate * first.d : 0.0f;
+      for (int i = l + L; i < a.k; i += L) dot += experts[i] >= 0 ? gates[i] * d_gates[i] : 0.0f;
+      dot = W::reduce(dot, Sum());
       order_lanes();
-      for (int i = l; i < a.k; i += 16) {
-        const int e = experts[i];
-        if (e >= 0) mine[e] += gates[i] * (d_gates[i] - dot);
-      }
+      if (first.expert >= 0) mine[first.expert] += first.gate * (first.d - dot);
+      for (int i = l + L; i < a.k; i += L)
+        if (experts[i] >= 0) mine[experts[i]] += gates[i] * (d_gates[i] - dot);
       order_lanes();
 #pragma unroll
-      for (int j = 0; j < R; ++j) d[j] = mine[l + 16 * j];
+      for (int j = 0; j < R; ++j) d[j] = mine[W::expert(l, j)];
     }
     char* to = static_cast<char*>(a.d_logits) + row * a.ld_d_logits * (a.logits_type == WB_F32 ? 4 : 2);
+    if constexpr (R == 1) {
+      if (l < a.num_experts) store_one(to, l, a.logits_type, routed ? d[0] : 0.0f);
+    } else {
 #pragma unroll
-    for (int j = 0; j < R; ++j)
-      if (l + 16 * j < a.num_experts) store_one(to, l + 16 * j, a.logits_type, routed ? d[j] : 0.0f);
+      for (int j = 0; j < R; j += 4) {
+        const int e = W::expert(l, j);
+        float v[4];
+        for (int i = 0; i < 4; ++i) v[i] = routed ? d[j + i] : 0.0f;
+        if (e + 4 <= a.num_experts) {
+          store_four(to, e, a.logits_type, v);
+        } else {
+          for (int i = 0; i < 4; ++i)
+            if (e + i < a.num_experts) store_one(to, e + i, a.logits_type, v[i]);
+        }
+      }
+    }
   }
 }
 
@@ -411,16 +532,16 @@ __global__ __launch_bounds__(kCombineThreads) void wb_combine_kernel(CombineArgs
     store_tail(out, c, a.cols, a.out_type, sum);
 }
 
-// Registers per lane for a row of E experts.
+// How a row of E experts lies over lanes and registers.
 template <class F>
 hipError_t by_width(int experts, F&& f) {
-  const int r = (experts + 15) / 16;
-  if (r <= 1) return f(std::integral_constant<int, 1>());
-  if (r <= 4) return f(std::integral_constant<int, 4>());
-  if (r <= 8) return f(std::integral_constant<int, 8>());
-  if (r <= 16) return f(std::integral_constant<int, 16>());
-  if (r <= 32) return f(std::integral_constant<int, 32>());
-  return f(std::integral_constant<int, 64>());
+  if (experts <= 8) return f(Row<8, 1>());
+  if (experts <= 32) return f(Row<8, 4>());
+  if (experts <= 64) return f(Row<8, 8>());
+  if (experts <= 128) return f(Row<8, 16>());
+  if (experts <= 256) return f(Row<8, 32>());
+  if (experts <= 512) return f(Row<16, 32>());
+  return f(Row<16, 64>());
 }
 
 }  // namespace
@@ -434,16 +555,16 @@ int launch_route(const RouteArgs& a, void* stream) {
   const auto st = static_cast<hipStream_t>(stream);
   const int64_t per = rows_per_block(a.rows), blocks = (a.rows + per - 1) / per;
   return by_width(a.num_experts, [&](auto width) {
-    constexpr int R = decltype(width)::value;
+    using W = decltype(width);
     if (blocks <= 1) {
-      hipLaunchKernelGGL((wb_route_few_kernel<R>), dim3(1), dim3(route_threads(R)), 0, st, a, per);
+      hipLaunchKernelGGL((wb_route_few_kernel<W>), dim3(1), dim3(W::T), 0, st, a, per);
       return hipGetLastError();
     }
     const uint32_t n = static_cast<uint32_t>(blocks);
-    hipLaunchKernelGGL((wb_route_kernel<R>), dim3(n), dim3(route_threads(R)), 0, st, a, blocks, per);
+    hipLaunchKernelGGL((wb_route_kernel<W>), dim3(n), dim3(W::T), 0, st, a, blocks, per);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((wb_route_place_kernel<R>), dim3(n + 1), dim3(route_threads(R)), 0, st, a, blocks, per);
+    hipLaunchKernelGGL((wb_route_place_kernel<W>), dim3(n + 1), dim3(kPlaceThreads), 0, st, a, blocks, per);
     return hipGetLastError();
   });
 }
@@ -451,9 +572,10 @@ int launch_route(const RouteArgs& a, void* stream) {
 int launch_route_grad(const RouteGradArgs& a, void* stream) {
   if (a.rows == 0) return hipSuccess;
   const auto st = static_cast<hipStream_t>(stream);
-  const int64_t blocks = std::min<int64_t>((a.rows + kGradThreads / 16 - 1) / (kGradThreads / 16), kGradBlocks);
   return by_width(a.num_experts, [&](auto width) {
-    hipLaunchKernelGGL((wb_route_grad_kernel<decltype(width)::value>), dim3(static_cast<uint32_t>(blocks)),
+    using W = decltype(width);
+    const int64_t per = kGradThreads / W::L, blocks = std::min<int64_t>((a.rows + per - 1) / per, kGradBlocks);
+    hipLaunchKernelGGL((wb_route_grad_kernel<W>), dim3(static_cast<uint32_t>(blocks)),
                        dim3(kGradThreads), 0, st, a);
     return hipGetLastError();
   });
