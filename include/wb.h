@@ -558,7 +558,8 @@ int wb_diff2_carry(const wb_field* fields, int32_t n, int32_t pass, int32_t last
  *   - A wb_matrix is rows x cols elements, a row `ld` elements (>= cols) after
  *     the one before it. Rows and pointers may lie at any multiple of the
  *     element size (the 16 bytes asked for above do not hold here). At most
- *     4194303 rows; matrices may have no rows, but have at least one column.
+ *     4194303 rows and 2^26 columns; matrices may have no rows, but have at
+ *     least one column.
  *   - Sums, norms, softmax and scales are computed in fp32 and rounded once to
  *     the output's type, to nearest even. NaN and infinities go through as the
  *     formulas have it; they stay in their rows.
@@ -630,8 +631,8 @@ typedef enum wb_activation { WB_ACT_NONE = 0, WB_ACT_SILU = 1, WB_ACT_GELU = 2 }
  *     be the residual itself.
  * With num_experts > 0 the weights are stacked: weight.rows = num_experts * N
  * rows, weight_scales.rows = num_experts * ceil(N/128), bias [num_experts, N].
- * offsets [num_experts + 1] (device): row p of out belongs to the expert with
- * offsets[e] <= p < offsets[e+1]; rows that belong to none are not written
+ * offsets [num_experts + 1] (device, ascending): row p of out belongs to the
+ * expert with offsets[e] <= p < offsets[e+1]; rows that belong to none are not written
  * (offsets are clamped to the rows of out). tokens [rows of out] (device, or
  * NULL): row p comes from row tokens[p] of x (clamped to its rows), else from
  * row p. Without experts offsets and tokens are NULL, and out has x's rows.

@@ -16,7 +16,7 @@ using wb::KnownRange;
 using wb::set_error;
 
 constexpr int64_t kMaxRows = 4194303;            // a row may take a workgroup of 1024 threads: 2^32 in a launch
-constexpr int64_t kMaxCols = int64_t(1) << 28;
+constexpr int64_t kMaxCols = int64_t(1) << 26;  // 2048 to a workgroup in y of a launch
 constexpr int64_t kMaxStride = int64_t(1) << 40;
 
 bool is_float(int32_t t) { return t == WB_F32 || t == WB_BF16; }
@@ -124,7 +124,7 @@ int check_linear(const wb_linear_args* p, Operands& ops, wb::LinearArgs& a, bool
   const int64_t e = stacked ? p->num_experts : 1, k = p->x.cols;
   if (p->weight.rows < 1 || p->weight.rows % e != 0) return set_error(WB_EINVAL, "weight rows are no multiple of num_experts");
   const int64_t n = p->weight.rows / e;
-  if (n > kMaxCols) return set_error(WB_EUNSUPPORTED, "weight of more than 2^28 rows");
+  if (n > kMaxCols) return set_error(WB_EUNSUPPORTED, "weight of more than 2^26 rows");
   if (p->gated && n % 2 != 0) return set_error(WB_EINVAL, "gated weight with an odd number of rows");
   const int64_t n_out = p->gated ? n / 2 : n, rows = stacked ? p->out.rows : p->x.rows;
   if (stacked && !p->tokens && p->x.rows != rows)

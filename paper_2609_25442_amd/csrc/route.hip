@@ -20,7 +20,7 @@
 // Places in expert order need every row's choice first: two launches, the
 // first over blocks of rows (choices, gates, and per block the counts and the
 // sums of p), the second over the same blocks (places) and one more (totals
-// and loss). Sums run over the blocks in their order and counts are integers,
+// and loss). Sums are taken in a fixed order and counts are integers,
 // so results do not depend on which workgroup ran first. Few rows take one
 // workgroup and one launch.
 #include <algorithm>

@@ -9,6 +9,7 @@ float32, bfloat16 or float8_e4m3fn in the memory of the current device; rows
 may lie any distance apart. fp8 activations go with float32 scales of one row
 and 128 columns, [rows, ceil(cols / 128)]; fp8 weights with those of 128x128
 blocks, as unpacking writes them. Arguments that do not fit raise WbError.
+Only ``route`` has a gradient: the others serve a rollout rank's tensors.
 """
 
 from __future__ import annotations
