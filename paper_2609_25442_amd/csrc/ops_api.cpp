@@ -18,6 +18,7 @@ using wb::set_error;
 constexpr int64_t kMaxRows = 4194303;            // a row may take a workgroup of 1024 threads: 2^32 in a launch
 constexpr int64_t kMaxCols = int64_t(1) << 26;  // 2048 to a workgroup in y of a launch
 constexpr int64_t kMaxStride = int64_t(1) << 40;
+constexpr int64_t kMaxExtent = int64_t(1) << 50;  // rows times row distance: bytes and offsets stay within 63 bits
 
 bool is_float(int32_t t) { return t == WB_F32 || t == WB_BF16; }
 int64_t type_bytes(int32_t t) { return t == WB_F32 ? 4 : t == WB_BF16 ? 2 : 1; }
@@ -47,7 +48,7 @@ struct Operands {
              std::to_string(rows) + " x " + std::to_string(cols));
       return;
     }
-    if (rows < 0 || cols < 1 || cols > kMaxCols || m.ld < cols || m.ld > kMaxStride) {
+    if (rows < 0 || cols < 1 || cols > kMaxCols || m.ld < cols || m.ld > kMaxStride || rows > kMaxExtent / m.ld) {
       refuse(std::string(name) + ": sizes or row distance out of range");
       return;
     }

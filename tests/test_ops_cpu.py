@@ -71,6 +71,19 @@ def test_linear_refuses(more, code):
     assert wb.lib.wb_linear(ctypes.byref(a), None, ctypes.c_size_t(0), None) == code
 
 
+@pytest.mark.parametrize("more", [
+    # extents whose bytes wrap around 64 bits to a few, or to none
+    dict(x=m((1 << 21) + 1, 64, ld=1 << 40), out=m((1 << 21) + 1, 32)),
+    dict(out=m((1 << 21) + 1, 32, ld=1 << 40), x=m((1 << 21) + 1, 64)),
+    dict(weight=m(1 << 23, 64, ld=1 << 40), out=m(4, 1 << 23)),
+    dict(weight=m(1 << 41, 64, ld=1 << 40), num_experts=1 << 15, offsets=4096, out=m(4, 1 << 26)),
+])
+def test_linear_refuses_extents_past_64_bits(more):
+    a = linear(**more)
+    assert workspace(a)[0] == wb.WB_EINVAL
+    assert b"out of range" in wb.lib.wb_last_error()
+
+
 def test_linear_refuses_memory_the_gpu_cannot_address():
     buf = ctypes.create_string_buffer(1 << 16)
     at = (ctypes.addressof(buf) + 255) // 256 * 256
