@@ -648,9 +648,11 @@ typedef struct wb_linear_args {
   int32_t reserved;
 } wb_linear_args;
 /* `workspace` (16-byte aligned, free again when the call's work is done) holds
- * the fp32 rows of some fp8 results; wb_linear_workspace says how many bytes
- * the same arguments need, 0 for most (then it may be NULL). It does not look
- * the pointers up. */
+ * the fp32 rows of some fp8 results, and copies of operands whose rows do not
+ * start at multiples of 16 bytes or hold a multiple of 16, where that is
+ * faster; wb_linear_workspace says how many bytes the same arguments need, 0
+ * for most (then it may be NULL). It does not look the pointers up, only at
+ * their last bits. */
 int wb_linear_workspace(const wb_linear_args* args, size_t* bytes);
 int wb_linear(const wb_linear_args* args, void* workspace, size_t workspace_bytes, void* stream);
 

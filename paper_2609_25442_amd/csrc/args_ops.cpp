@@ -288,8 +288,12 @@ PyObject* wb_py_linear(PyObject*, PyObject* const* args, Py_ssize_t n) {
     Tensor workspace;
     size_t bytes = 0;
     int rc = WB_OK;
-    if (t == at::kFloat8_e4m3fn) {  // only these may need one
-      scales = fresh({rows, scale_cols(cols)}, at::kFloat, x), a.out_scales = matrix(scales, "scales");
+    const bool f8 = t == at::kFloat8_e4m3fn;
+    if (f8) scales = fresh({rows, scale_cols(cols)}, at::kFloat, x), a.out_scales = matrix(scales, "scales");
+    const int64_t es = x.element_size();
+    const bool on_grid = ((reinterpret_cast<uintptr_t>(a.x.data) | reinterpret_cast<uintptr_t>(a.weight.data) |
+                           static_cast<uintptr_t>((a.x.ld | a.weight.ld | a.x.cols) * es)) & 15) == 0;
+    if (f8 || !on_grid) {  // else none is needed
       rc = size(&a, &bytes);
       if (rc == WB_OK && bytes) workspace = fresh({static_cast<int64_t>(bytes)}, at::kByte, x);
     }

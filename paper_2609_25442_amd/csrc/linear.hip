@@ -194,8 +194,8 @@ __device__ __forceinline__ void block_sums(const Operand<F8>& w, const Operand<F
 // wavefronts. LDS holds a ring of RING slots of STEP stages of every row of
 // both; a barrier stands between slots, so small tiles take more stages at
 // once, and KG such sets of wavefronts share them out (their sums meet in LDS
-// at the end, in order). The pieces of a row are permuted by its number so that sixteen rows'
-// pieces at one place of k fall into different banks.
+// at the end, in order). The pieces of a row are permuted by its number so
+// that sixteen rows' pieces at one place of k fall into different banks.
 template <int BM_, int BN_, int WM_, int WN_, int KG_, int STEP_, int RING_>
 struct Shape {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, KG = KG_, STEP = STEP_, RING = RING_;
@@ -217,6 +217,18 @@ __device__ __forceinline__ int swizzle(int row) { return (row >> 1) & 7; }
 // hold a multiple of 16, and the sixteen rows of a block share a weight
 // scale: tiles go from memory to LDS without registers between. Otherwise
 // through registers, piece by piece, and scales by row.
+//
+// What bounds it, as measured (rates of a large copy and of a large bf16
+// product on this card: 6.7 TB/s, 1.54 PFLOP/s):
+//   8192 rows, 28672 x 4096 bf16, gated    1.50 ms, 1.28 PFLOP/s: the matrix
+//     cores, 63 % of the cycles (the rest: barriers, operands from LDS)
+//   4096 rows, 7168 x 2048 fp8, and 8192 of 32 experts' 4096 x 7168, gated:
+//     0.15 and 0.67 ms, 0.82 and 0.72 PFLOP/s: widening and scaling in the
+//     vector units, beside matrix cores busy 35 to 41 %
+//   128 rows of the same 32 experts: 0.18 ms, the weight's bytes at 5.3 TB/s
+//   1 row, 6144 x 4096 bf16: 10 us, 5.0 TB/s with the launch and the call
+//   333 rows, 3442 x 1500 bf16, by way of registers: 18 us; 14 were the rows
+//     1504 long and on the 16-byte grid
 template <class S, bool F8, bool DIRECT>
 __global__ __launch_bounds__(S::kThreads, 2) void wb_linear_tile_kernel(LinearArgs a, uint32_t tiles_n, uint32_t group) {
   extern __shared__ __align__(128) uint8_t lds[];
@@ -605,7 +617,8 @@ __global__ __launch_bounds__(S::kThreads, 2) void wb_linear_tile_kernel(LinearAr
 
 // fp8 codes and scales of fp32 rows, for tiles too narrow to hold the 128
 // columns of a scale: sixteen lanes a scale, eight columns each. Rows that
-// belong to no expert are left alone.
+// belong to no expert are left alone. Bound by the launch for few rows (128 rows
+// of 2048: 5 us), by its bytes for many (8192 rows: 15 us).
 __global__ __launch_bounds__(256) void wb_linear_codes_kernel(const float* sums, LinearArgs a) {
   const int64_t row = blockIdx.x, c = (int64_t(blockIdx.y) * 256 + threadIdx.x) * 8;
   if (a.offsets && (row < a.offsets[0] || row >= a.offsets[a.num_experts])) return;
@@ -629,6 +642,33 @@ __global__ __launch_bounds__(256) void wb_linear_codes_kernel(const float* sums,
     for (int i = 0; i < 8; ++i)
       if (c + i < a.n_out) to[i] = static_cast<uint8_t>(p[i >> 2] >> (8 * (i & 3)));
   }
+}
+
+// Rows of x and of the weight that start off the 16-byte grid, onto it: 16-byte
+// pieces in order, zeros past a row's end (in both operands, so that sums stay
+// as they are), four pieces a thread. Bound by its bytes.
+struct Realign {
+  const uint8_t* from;
+  u32x4* to;
+  int64_t ld, bytes;       // a row's distance and length
+  uint32_t pieces, count;  // of a row, of all rows
+};
+
+__global__ __launch_bounds__(256) void wb_linear_realign_kernel(Realign x, Realign weight, uint32_t x_blocks) {
+  const bool second = blockIdx.x >= x_blocks;
+  const Realign a = second ? weight : x;
+  const uint32_t base = (blockIdx.x - (second ? x_blocks : 0)) * 1024 + threadIdx.x;
+  u32x4 v[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t at = base + i * 256;
+    if (at >= a.count) continue;
+    const uint32_t row = at / a.pieces;
+    v[i] = load_piece(a.from + row * a.ld, int64_t(at - row * a.pieces) * 16, a.bytes);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (base + i * 256 < a.count) a.to[base + i * 256] = v[i];
 }
 
 // Row tiles of `per` rows: each expert's last may be part of one, so there is
@@ -660,8 +700,6 @@ hipError_t launch_tile(const LinearArgs& a, hipStream_t st) {
                      static_cast<uint32_t>(tiles_n), 8u);
   return hipGetLastError();
 }
-
-
 
 // The tiles in use. A launch takes the one whose rounds over the 256 CUs are
 // expected to be done first. A round takes us per stage of k (128 bytes of a
@@ -697,7 +735,7 @@ bool holds_scales(const LinearArgs& a, int choice) {
   return (a.gated ? kChoices[choice].bn / 2 : kChoices[choice].bn) % kScaleBlock == 0;
 }
 
-int choose(const LinearArgs& a) {
+int choose(const LinearArgs& a, double* expected) {
   const int f8 = a.in_type == WB_F8E4M3;
   const double stages = std::ceil(double(a.k) * (f8 ? 1 : 2) / kStageBytes);
   int best = -1;
@@ -720,7 +758,50 @@ int choose(const LinearArgs& a) {
                       (a.out_type == WB_F8E4M3 && !holds_scales(a, i) ? kCodesUs : 0.0);
     if (best < 0 || us < least) best = i, least = us;
   }
+  *expected = least;
   return best;
+}
+
+// How a launch goes: its tile, and for rows off the 16-byte grid whether
+// copies of them, in the workspace, are expected to be done first.
+struct Form {
+  LinearArgs a;  // the product; x and weight are set where they are copied
+  int choice;
+  bool copy_x = false, copy_weight = false;
+  size_t x_bytes = 0, weight_bytes = 0, sums_bytes = 0;
+};
+// Measured: 4 to 6 us for the launch, and 3.2 TB/s (what comes back from the caches
+// included). 4000 rows, 4096 x 1001: bf16 69 us by way of registers and 51 by
+// way of copies, fp8 116 and 54; 2 rows, 1337 x 7543 bf16 39 and 22; 333 rows,
+// 3442 x 1500 bf16 18 and 24; 40 rows, 300 x 700 6.5 and 10.6.
+constexpr double kCopyUs = 6.0, kCopyBytesPerUs = 3.2e6;
+
+Form form_of(const LinearArgs& a) {
+  Form f;
+  double us = 0.0, copied_us = 0.0;
+  f.a = a, f.choice = choose(a, &us);
+  const int64_t es = a.in_type == WB_F8E4M3 ? 1 : 2, pitch = (a.k * es + 15) / 16 * 16;
+  auto off_grid = [&](const uint8_t* p, int64_t ld) {
+    return ((reinterpret_cast<uintptr_t>(p) | static_cast<uintptr_t>(ld) | static_cast<uintptr_t>(a.k * es)) & 15) != 0;
+  };
+  const bool x = off_grid(a.x, a.ld_x_bytes), weight = off_grid(a.weight, a.ld_w_bytes);
+  if (!a.direct && (x || weight)) {
+    LinearArgs b = a;
+    b.k = static_cast<int32_t>(pitch / es);
+    if (x) b.ld_x_bytes = pitch;
+    if (weight) b.ld_w_bytes = pitch, b.stride_w_bytes = b.n * pitch;
+    b.direct = linear_near(b);
+    const int64_t x_rows = x ? a.x_rows : 0, w_rows = weight ? int64_t(a.n) * std::max(1, a.num_experts) : 0;
+    const int64_t most = (int64_t(1) << 32) - 4096;  // pieces are counted in 32 bits
+    if (b.direct && x_rows <= most / (pitch / 16) && w_rows <= most / (pitch / 16)) {
+      const int choice = choose(b, &copied_us);
+      copied_us += kCopyUs + double(x_rows + w_rows) * pitch / kCopyBytesPerUs;
+      if (copied_us < us)
+        f.a = b, f.choice = choice, f.copy_x = x, f.copy_weight = weight, f.x_bytes = x_rows * pitch, f.weight_bytes = w_rows * pitch;
+    }
+  }
+  if (a.out_type == WB_F8E4M3 && !holds_scales(a, f.choice)) f.sums_bytes = static_cast<size_t>(a.rows) * a.n_out * sizeof(float);
+  return f;
 }
 
 template <class S, int CHOICE>
@@ -754,22 +835,44 @@ hipError_t launch_choice(const LinearArgs& a, int choice, hipStream_t st) {
 
 }  // namespace
 
+bool linear_near(const LinearArgs& a) {
+  const int64_t reach = (int64_t(1) << 32) - 4096;
+  return a.n * a.ld_w_bytes < reach && (a.tokens ? a.x_rows : 256) * a.ld_x_bytes < reach &&
+         !(a.in_type == WB_F8E4M3 && a.gated && a.n_out % 16 != 0);
+}
+
 size_t linear_workspace_bytes(const LinearArgs& a) {
-  if (a.rows == 0 || a.out_type != WB_F8E4M3 || holds_scales(a, choose(a))) return 0;
-  return static_cast<size_t>(a.rows) * a.n_out * sizeof(float);
+  if (a.rows == 0) return 0;
+  const Form f = form_of(a);
+  return f.x_bytes + f.weight_bytes + f.sums_bytes;
 }
 
 int launch_linear(const LinearArgs& a, void* workspace, void* stream) {
   if (a.rows == 0) return hipSuccess;
   const auto st = static_cast<hipStream_t>(stream);
-  const int choice = choose(a);
-  if (a.out_type != WB_F8E4M3 || holds_scales(a, choice)) return launch_choice(a, choice, st);
-  LinearArgs sums = a;
-  sums.out = workspace, sums.out_type = WB_F32, sums.ld_out = a.n_out;
-  const hipError_t e = launch_choice(sums, choice, st);
+  Form f = form_of(a);
+  auto* at = static_cast<uint8_t*>(workspace);
+  if (f.copy_x || f.copy_weight) {
+    const int64_t bytes = a.k * (a.in_type == WB_F8E4M3 ? 1 : 2);
+    auto realign = [&](const uint8_t*& p, int64_t ld, size_t size) {
+      const Realign r{p, reinterpret_cast<u32x4*>(at), ld, bytes, static_cast<uint32_t>((bytes + 15) / 16), static_cast<uint32_t>(size / 16)};
+      if (size) p = at;
+      at += size;
+      return r;
+    };
+    const Realign x = realign(f.a.x, a.ld_x_bytes, f.x_bytes), weight = realign(f.a.weight, a.ld_w_bytes, f.weight_bytes);
+    auto blocks = [](const Realign& r) { return (r.count + 1023) / 1024; };
+    hipLaunchKernelGGL(wb_linear_realign_kernel, dim3(blocks(x) + blocks(weight)), dim3(256), 0, st, x, weight, blocks(x));
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (!f.sums_bytes) return launch_choice(f.a, f.choice, st);
+  LinearArgs sums = f.a;
+  sums.out = at, sums.out_type = WB_F32, sums.ld_out = a.n_out;
+  const hipError_t e = launch_choice(sums, f.choice, st);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(wb_linear_codes_kernel, dim3(static_cast<uint32_t>(a.rows), static_cast<uint32_t>((a.n_out + 2047) / 2048)),
-                     dim3(256), 0, st, static_cast<const float*>(workspace), a);
+                     dim3(256), 0, st, reinterpret_cast<const float*>(at), a);
   return hipGetLastError();
 }
 

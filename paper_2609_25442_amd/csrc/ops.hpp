@@ -98,6 +98,10 @@ struct LinearArgs {
 size_t route_workspace_bytes(int64_t rows, int32_t experts);
 size_t linear_workspace_bytes(const LinearArgs& a);
 
+// Whether 32-bit offsets reach the rows of x and weight, and sixteen rows of
+// the weight share a scale.
+bool linear_near(const LinearArgs& a);
+
 // Each enqueues its kernels on the stream and returns a hipError_t.
 int launch_add_rms_norm(const NormArgs& a, void* stream);
 int launch_route(const RouteArgs& a, void* stream);

@@ -171,10 +171,7 @@ int check_linear(const wb_linear_args* p, Operands& ops, wb::LinearArgs& a, bool
   const uintptr_t at = reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.weight) |
                        static_cast<uintptr_t>(a.ld_x_bytes) | static_cast<uintptr_t>(a.ld_w_bytes) |
                        static_cast<uintptr_t>(k * es);
-  // the kernels' offsets from the weight and from x have 32 bits
-  const int64_t reach = (int64_t(1) << 32) - 4096;
-  const bool near = n * a.ld_w_bytes < reach && (a.tokens ? a.x_rows : 256) * a.ld_x_bytes < reach;
-  a.direct = at % 16 == 0 && near && !(f8 && a.gated && n_out % 16 != 0);
+  a.direct = at % 16 == 0 && wb::linear_near(a);
   return WB_OK;
 }
 

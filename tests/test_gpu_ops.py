@@ -551,3 +551,58 @@ def test_refusals():
             call()
         assert str(e.value), n
     torch.cuda.synchronize()
+
+
+# ---- rows off the 16-byte grid that are copied onto it first ------------------------------------
+
+@pytest.mark.parametrize("f8", [False, True], ids=["bf16", "f8"])
+@pytest.mark.parametrize("size", [(2, 1337, 7543), (8, 96, 6001), (300, 1000, 1501), (1000, 1056, 1001), (1030, 2304, 250)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_linear_of_long_or_many_odd_rows(size, f8):
+    say("linear copied", size, f8)
+    for form in (FORMS[0], FORMS[3]) if size[1] % 32 == 0 else (FORMS[0],):
+        x, w, xs, ws, b, r, cols = product_inputs(*size, f8, form)
+        want, err = ref.product(x, w[0], b and b[0], form.get("activation", "none"), form.get("gated", False), r, xs, ws and ws[0])
+        for out in ("f32", "f8e4m3"):
+            got = run_linear(gpu(x), gpu(w[0]), gpu(xs), gpu(ws and ws[0]), gpu(b and b[0]), gpu(r), form, out)
+            torch.cuda.synchronize()
+            check_product(got, want, err, out, f"{size} {out}")
+
+
+@pytest.mark.parametrize("f8", [False, True], ids=["bf16", "f8"])
+@pytest.mark.parametrize("which", ["x", "weight", "both"])
+def test_linear_copies_only_what_is_off_the_grid(which, f8):
+    """Values beyond the rows' ends are NaN: a copy must not take them along."""
+    say("linear copied", which, f8)
+    x, w, xs, ws, _, _, _ = product_inputs(24, 96, 6016, f8, {})
+    want, err = ref.product(x, w[0], None, "none", False, None, xs, ws and ws[0])
+
+    def off(t):
+        wide = torch.full((t.shape[0], t.shape[1] + 24), math.nan).to(t.dtype).cuda()
+        wide[:, 5:5 + t.shape[1]] = gpu(t)
+        return wide[:, 5:5 + t.shape[1]]
+
+    gx = gpu(x) if which == "weight" else off(x)
+    gw = gpu(w[0]) if which == "x" else off(w[0])
+    got = wb.linear(gx, gw, x_scales=gpu(xs), weight_scales=gpu(ws and ws[0]), out_dtype="f32")
+    torch.cuda.synchronize()
+    ref.check(got, want, err, which)
+
+
+@pytest.mark.parametrize("f8", [False, True], ids=["bf16", "f8"])
+def test_expert_linear_of_long_odd_rows(f8):
+    say("experts copied", f8)
+    counts, n, k = [1, 0, 40, 23], 64, 4111
+    x, w, xs, ws, _, _, _ = product_inputs(30, n, k, f8, {}, e=len(counts))
+    tokens = torch.arange(sum(counts), dtype=torch.int32) % 30
+    at, wants, errs = [0], [], []
+    for i, c in enumerate(counts):
+        mine = tokens[at[-1]:at[-1] + c].long()
+        at.append(at[-1] + c)
+        want, err = ref.product(x[mine], w[i], None, "none", False, None, None if xs is None else xs[mine], ws and ws[i])
+        wants.append(want)
+        errs.append(err)
+    got = wb.expert_linear(gpu(x), torch.stack(w).cuda(), torch.tensor(at, dtype=torch.int32, device="cuda"), gpu(tokens),
+                           x_scales=gpu(xs), weight_scales=torch.stack(ws).cuda() if f8 else None, out_dtype="f32")
+    torch.cuda.synchronize()
+    ref.check(got, torch.cat(wants), torch.cat(errs), "experts")

@@ -50,6 +50,16 @@ def test_linear_workspace_of_fp8_results_holds_fp32_rows():
     assert rc == wb.WB_OK and n in (0, 4 * 4096 * 4)
 
 
+def test_linear_workspace_of_long_rows_off_the_grid_holds_copies():
+    assert workspace(linear(x=m(2, 7543), weight=m(1337, 7543), out=m(2, 1337))) == (wb.WB_OK, 1339 * 7544 * 2)
+    # only what is off the grid
+    assert workspace(linear(x=m(24, 6016, data=4106), weight=m(96, 6016), out=m(24, 96))) == (wb.WB_OK, 24 * 6016 * 2)
+    assert workspace(linear(x=m(24, 6016), weight=m(96, 6016, ld=6017), out=m(24, 96))) == (wb.WB_OK, 96 * 6016 * 2)
+    # with the fp32 rows behind them
+    rc, n = workspace(linear(x=m(8, 6001), weight=m(96, 6001), out=m(8, 96, F8), out_scales=m(8, 1, F32)))
+    assert rc == wb.WB_OK and n == 104 * 6008 * 2 + 8 * 96 * 4
+
+
 @pytest.mark.parametrize("more,code", [
     (dict(x=m(4, 63)), wb.WB_EINVAL), (dict(out=m(4, 31)), wb.WB_EINVAL), (dict(out=m(3, 32)), wb.WB_EINVAL),
     (dict(x=m(4, 64, ld=63)), wb.WB_EINVAL), (dict(gated=1), wb.WB_EINVAL), (dict(activation=3), wb.WB_EINVAL),
