@@ -121,13 +121,29 @@ __device__ __forceinline__ u32x4 load_piece(const uint8_t* row, int64_t at, int6
   return v;
 }
 
-// Four neighbouring columns of a row; in: how many of them exist.
-__device__ __forceinline__ void load_four(const void* base, int64_t at, int type, int in, float (&v)[4]) {
+// Four neighbouring columns of a row as they lie in memory, and as numbers; in:
+// how many of them exist.
+__device__ __forceinline__ u32x4 fetch_four(const void* base, int64_t at, int type, int in) {
+  u32x4 v = {0, 0, 0, 0};
+  const auto* wide = static_cast<const float*>(base) + at;
+  const auto* half = static_cast<const uint16_t*>(base) + at;
   if (in >= 4) {
-    wb::load_four(base, at, type, v);
-  } else {
-    for (int r = 0; r < 4; ++r) v[r] = r < in ? load_one(base, at + r, type) : 0.0f;
+    if (type == WB_F32) return __builtin_bit_cast(u32x4, *reinterpret_cast<const f32x4_a4*>(wide));
+    const u32x2 u = *reinterpret_cast<const u32x2_a2*>(half);
+    return u32x4{u[0], u[1], 0, 0};
   }
+  for (int r = 0; r < 4; ++r) {
+    if (r >= in) continue;
+    if (type == WB_F32)
+      v[r] = __builtin_bit_cast(uint32_t, wide[r]);
+    else
+      v[r >> 1] |= uint32_t(half[r]) << (16 * (r & 1));
+  }
+  return v;
+}
+
+__device__ __forceinline__ float of_four(const u32x4& u, int type, int r) {
+  return __builtin_bit_cast(float, type == WB_F32 ? u[r] : r & 1 ? u[r >> 1] & 0xffff0000u : u[r >> 1] << 16);
 }
 
 __device__ __forceinline__ void store_four(void* base, int64_t at, int type, int in, const float (&v)[4]) {
@@ -490,30 +506,6 @@ __global__ __launch_bounds__(S::kThreads, 2) void wb_linear_tile_kernel(LinearAr
     }
   }
 
-  if constexpr (S::KG > 1) {
-    float* const sums = reinterpret_cast<float*>(lds);
-    const int own = (wave % (S::WM * S::WN) * S::FN * S::FM) * 256 + lane * 4;
-    __syncthreads();
-    if (kg > 0) {
-#pragma unroll
-      for (int i = 0; i < S::FN; ++i)
-#pragma unroll
-        for (int j = 0; j < S::FM; ++j)
-          *reinterpret_cast<f32x4*>(sums + (kg - 1) * S::BM * S::BN + own + (i * S::FM + j) * 256) = acc[i][j];
-    }
-    __syncthreads();
-    if (kg == 0) {
-#pragma unroll
-      for (int i = 0; i < S::FN; ++i)
-#pragma unroll
-        for (int j = 0; j < S::FM; ++j)
-          for (int g = 0; g < S::KG - 1; ++g) {
-            const f32x4 add = *reinterpret_cast<const f32x4*>(sums + g * S::BM * S::BN + own + (i * S::FM + j) * 256);
-            for (int r = 0; r < 4; ++r) acc[i][j][r] += add[r];
-          }
-    }
-  }
-
   // epilogue, sixteen rows at a time through LDS: a wavefront puts its sums
   // down by row and takes them up again four neighbouring columns per lane, a
   // row by neighbouring lanes, which is also how they are stored
@@ -536,44 +528,73 @@ __global__ __launch_bounds__(S::kThreads, 2) void wb_linear_tile_kernel(LinearAr
       if (a.gated) bias_up[e] = load_bias(a, rows.expert, a.n_out + b);
     }
   }
-  // Four of the lane's rows of block j at a time. The residual's loads come
-  // first, and only where there is one: a wait for loads is one for the
-  // stores before them as well.
+  // The residual's loads are some of the lane's rows ahead, and in front
+  // of the stores: a wait for loads is one for the stores before them as well.
+  auto residual_of = [&](int j, int r) {
+    return fetch_four(a.residual, (m0 + min(j * 16 + r, there - 1)) * a.ld_residual + col, a.residual_type, in_row);
+  };
+  constexpr int kAhead = S::FN > 4 ? 2 : S::FN;  // more spill, of the largest tile
+  u32x4 add[kAhead];
+  if (a.residual && there > 0) {
+#pragma unroll
+    for (int h = 0; h < kAhead; ++h)
+      if (first_r + h * per < 16) add[h] = residual_of(0, first_r + h * per);
+  }
+
+  if constexpr (S::KG > 1) {
+    float* const sums = reinterpret_cast<float*>(lds);
+    const int own = (wave % (S::WM * S::WN) * S::FN * S::FM) * 256 + lane * 4;
+    __syncthreads();
+    if (kg > 0) {
+#pragma unroll
+      for (int i = 0; i < S::FN; ++i)
+#pragma unroll
+        for (int j = 0; j < S::FM; ++j)
+          *reinterpret_cast<f32x4*>(sums + (kg - 1) * S::BM * S::BN + own + (i * S::FM + j) * 256) = acc[i][j];
+    }
+    __syncthreads();
+    if (kg == 0) {
+#pragma unroll
+      for (int i = 0; i < S::FN; ++i)
+#pragma unroll
+        for (int j = 0; j < S::FM; ++j)
+          for (int g = 0; g < S::KG - 1; ++g) {
+            const f32x4 more = *reinterpret_cast<const f32x4*>(sums + g * S::BM * S::BN + own + (i * S::FM + j) * 256);
+            for (int r = 0; r < 4; ++r) acc[i][j][r] += more[r];
+          }
+    }
+  }
+
   auto finish_rows = [&](int j, auto with_residual) {
-#pragma unroll 1
-    for (int r0 = first_r; r0 < 16; r0 += 4 * per) {
-      float add[4][4];
-      if constexpr (with_residual) {
 #pragma unroll
-        for (int h = 0; h < 4; ++h) {
-          const int r = j * 16 + r0 + h * per;
-          load_four(a.residual, (m0 + min(r, there - 1)) * a.ld_residual + col, a.residual_type, in_row, add[h]);
-        }
+    for (int h = 0; h < S::FN; ++h) {
+      const int r = first_r + h * per;
+      if (r >= 16) break;
+      const int in = j * 16 + r < there ? in_row : 0;
+      float* p = mine + r * kPitch + at;
+      const f32x4 g = *reinterpret_cast<const f32x4*>(p);
+      float v[4];
+      if (a.gated) {
+        const f32x4 u = *reinterpret_cast<const f32x4*>(p + 16);
+        for (int e = 0; e < 4; ++e) v[e] = activate(g[e] + bias[e], a.activation) * (u[e] + bias_up[e]);
+      } else {
+        for (int e = 0; e < 4; ++e) v[e] = activate(g[e] + bias[e], a.activation);
       }
-#pragma unroll
-      for (int h = 0; h < 4; ++h) {
-        const int r = r0 + h * per;
-        if (r >= 16) break;
-        const int in = j * 16 + r < there ? in_row : 0;
-        float* p = mine + r * kPitch + at;
-        const f32x4 g = *reinterpret_cast<const f32x4*>(p);
-        float v[4];
-        if (a.gated) {
-          const f32x4 u = *reinterpret_cast<const f32x4*>(p + 16);
-          for (int e = 0; e < 4; ++e) v[e] = activate(g[e] + bias[e], a.activation) * (u[e] + bias_up[e]);
-        } else {
-          for (int e = 0; e < 4; ++e) v[e] = activate(g[e] + bias[e], a.activation);
-        }
-        if constexpr (with_residual)
-          for (int e = 0; e < 4; ++e) v[e] += add[h][e];
-        if (f8_out) {
-          *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
-          float top = largest(v, in, 0.0f);
-          for (int off = lanes / 2; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
-          if (c == 0) tops[wn * S::BM + wm * S::TM + j * 16 + r] = top;
-        } else if (in > 0) {
-          store_four(a.out, (m0 + j * 16 + r) * a.ld_out + col, a.out_type, in, v);
-        }
+      if constexpr (with_residual) {
+        u32x4& of_row = add[h % kAhead];
+        for (int e = 0; e < 4; ++e) v[e] += of_four(of_row, a.residual_type, e);
+        if (r + kAhead * per < 16)
+          of_row = residual_of(j, r + kAhead * per);
+        else if (j + 1 < S::FM)
+          of_row = residual_of(j + 1, first_r + h % kAhead * per);
+      }
+      if (f8_out) {
+        *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
+        float top = largest(v, in, 0.0f);
+        for (int off = lanes / 2; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
+        if (c == 0) tops[wn * S::BM + wm * S::TM + j * 16 + r] = top;
+      } else if (in > 0) {
+        store_four(a.out, (m0 + j * 16 + r) * a.ld_out + col, a.out_type, in, v);
       }
     }
   };
