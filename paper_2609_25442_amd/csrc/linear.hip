@@ -239,7 +239,7 @@ __device__ __forceinline__ int swizzle(int row) { return (row >> 1) & 7; }
 //   8192 rows, 28672 x 4096 bf16, gated    1.50 ms, 1.28 PFLOP/s: the matrix
 //     cores, 63 % of the cycles (the rest: barriers, operands from LDS)
 //   4096 rows, 7168 x 2048 fp8, and 8192 of 32 experts' 4096 x 7168, gated:
-//     0.15 and 0.67 ms, 0.82 and 0.72 PFLOP/s: widening and scaling in the
+//     0.14 and 0.67 ms, 0.88 and 0.72 PFLOP/s: widening and scaling in the
 //     vector units, beside matrix cores busy 35 to 41 %
 //   128 rows of the same 32 experts: 0.18 ms, the weight's bytes at 5.3 TB/s
 //   1 row, 6144 x 4096 bf16: 10 us, 5.0 TB/s with the launch and the call
@@ -529,7 +529,8 @@ __global__ __launch_bounds__(S::kThreads, 2) void wb_linear_tile_kernel(LinearAr
     }
   }
   // The residual's loads are some of the lane's rows ahead, and in front
-  // of the stores: a wait for loads is one for the stores before them as well.
+  // of the stores: a wait for loads is one for the stores before them as well
+  // (4096 rows by 7168 x 2048 fp8: 133 us, 142 with the loads in between).
   auto residual_of = [&](int j, int r) {
     return fetch_four(a.residual, (m0 + min(j * 16 + r, there - 1)) * a.ld_residual + col, a.residual_type, in_row);
   };
@@ -729,8 +730,8 @@ hipError_t launch_tile(const LinearArgs& a, hipStream_t st) {
 // has a CU to itself), for bf16 and fp8; the last two are us, with 512 and
 // with 256 tiles, of rows that come by way of registers (0: not in use). Large
 // tiles read less per product; small ones give every CU work, and keep more of
-// the weight on its way when few rows meet it. 8192 x 8192 x 8192 bf16: 0.84
-// ms with 256 x 256, 0.95 with 128 x 128; 1024 x 7168 x 2048 fp8: 77 us and 43;
+// the weight on its way when few rows meet it. 8192 x 8192 x 8192 bf16: 0.85
+// ms with 256 x 256, 0.99 with 128 x 128; 1024 x 7168 x 2048 fp8: 67 us and 37;
 // one row by 6144 x 4096 bf16: 12 us with 16 x 32, 31 with 64 x 64.
 struct Choice {
   int bm, bn, resident;
