@@ -613,8 +613,10 @@ int wb_route(const wb_matrix* logits, const uint8_t* mask, int32_t k, int32_t re
 /* Gradient of the logits from those of the gates [T, k] and of the loss [1]
  * (WB_F32 device pointers, either may be NULL: zero). logits, mask, k and
  * renormalize as given to wb_route, `routing` what it wrote (experts, gates,
- * counts and routed are read). d_logits has the logits' type and shape; it may be logits
- * itself. The choice of experts has no gradient. Errors as wb_route. */
+ * counts and routed are read; an expert outside 0..E-1 is a choice of none, as -1
+ * is, and a row's experts are different ones). d_logits has the logits' type and
+ * shape; it may be logits itself. The choice of experts has no gradient. Errors as
+ * wb_route. */
 int wb_route_backward(const wb_matrix* logits, const uint8_t* mask, int32_t k, int32_t renormalize,
                       const wb_routing* routing, const float* d_gates, const float* d_loss,
                       const wb_matrix* d_logits, void* stream);

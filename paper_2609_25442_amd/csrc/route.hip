@@ -406,7 +406,8 @@ __global__ __launch_bounds__(W::T) void wb_route_few_kernel(RouteArgs a, int64_t
 
 // What the gates add at a row's choices goes through the
 // row's copy in LDS, lane i adding choice i's (the choices are different
-// experts): k times R selections between registers take longer.
+// experts): k times R selections between registers take longer. A choice that
+// is no expert's number is none, as -1 is: it has no place in the copy.
 template <class W>
 __global__ __launch_bounds__(kGradThreads) void wb_route_grad_kernel(RouteGradArgs a) {
   constexpr int R = W::R, L = W::L, kGroups = kGradThreads / L, kPitch = W::E + 1;
@@ -429,6 +430,7 @@ __global__ __launch_bounds__(kGradThreads) void wb_route_grad_kernel(RouteGradAr
       int32_t expert;
       float gate, d;
     } first = {-1, 0.0f, 0.0f};
+    auto there = [&](int32_t e) { return static_cast<uint32_t>(e) < static_cast<uint32_t>(a.num_experts); };
     if (a.d_gates && l < a.k) first = {a.experts[row * a.k + l], a.gates[row * a.k + l], a.d_gates[row * a.k + l]};
     const bool masked = a.mask && !a.mask[row];
     load_logits<W>(a.logits, row, a.ld_logits, a.logits_type, a.num_experts, l, z);
@@ -442,9 +444,9 @@ __global__ __launch_bounds__(kGradThreads) void wb_route_grad_kernel(RouteGradAr
 #pragma unroll
       for (int j = 0; j < R; ++j) mine[W::expert(l, j)] = d[j];
       order_lanes();
-      if (first.expert >= 0) mine[first.expert] += first.d;
+      if (there(first.expert)) mine[first.expert] += first.d;
       for (int i = l + L; i < a.k; i += L)
-        if (experts[i] >= 0) mine[experts[i]] += d_gates[i];
+        if (there(experts[i])) mine[experts[i]] += d_gates[i];
       order_lanes();
 #pragma unroll
       for (int j = 0; j < R; ++j) d[j] = mine[W::expert(l, j)];
@@ -458,13 +460,13 @@ __global__ __launch_bounds__(kGradThreads) void wb_route_grad_kernel(RouteGradAr
     if (d_gates && a.renormalize) {
 #pragma unroll
       for (int j = 0; j < R; ++j) mine[W::expert(l, j)] = d[j];
-      float dot = first.expert >= 0 ? first.gate * first.d : 0.0f;
-      for (int i = l + L; i < a.k; i += L) dot += experts[i] >= 0 ? gates[i] * d_gates[i] : 0.0f;
+      float dot = there(first.expert) ? first.gate * first.d : 0.0f;
+      for (int i = l + L; i < a.k; i += L) dot += there(experts[i]) ? gates[i] * d_gates[i] : 0.0f;
       dot = W::reduce(dot, Sum());
       order_lanes();
-      if (first.expert >= 0) mine[first.expert] += first.gate * (first.d - dot);
+      if (there(first.expert)) mine[first.expert] += first.gate * (first.d - dot);
       for (int i = l + L; i < a.k; i += L)
-        if (experts[i] >= 0) mine[experts[i]] += gates[i] * (d_gates[i] - dot);
+        if (there(experts[i])) mine[experts[i]] += gates[i] * (d_gates[i] - dot);
       order_lanes();
 #pragma unroll
       for (int j = 0; j < R; ++j) d[j] = mine[W::expert(l, j)];

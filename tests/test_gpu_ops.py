@@ -606,3 +606,23 @@ def test_expert_linear_of_long_odd_rows(f8):
                            x_scales=gpu(xs), weight_scales=torch.stack(ws).cuda() if f8 else None, out_dtype="f32")
     torch.cuda.synchronize()
     ref.check(got, torch.cat(wants), torch.cat(errs), "experts")
+
+
+# ---- integers that are no expert's number --------------------------------------------------------
+
+@pytest.mark.parametrize("shape", [(40, 8, 4), (70, 60, 17), (33, 256, 8), (9, 513, 20)], ids=lambda s: "x".join(map(str, s)))
+def test_route_gradient_leaves_out_choices_that_are_no_experts(shape):
+    """As if they were -1, bit for bit, in their own row and in its neighbours."""
+    say("route gradient, experts out of range", shape)
+    rows, e, k = shape
+    z = ref.randn(rows, e, seed=4).cuda()
+    d_gates, d_loss = ref.randn(rows, k, seed=5).cuda(), torch.tensor(0.5, device="cuda")
+    away = torch.rand(rows, k, generator=torch.Generator().manual_seed(6)).cuda() < 0.4
+    wrong = torch.tensor([e, e + 1, 2 * e, 1023, 1024, 1 << 20, 2 ** 31 - 1, -2, -2 ** 31], dtype=torch.int32, device="cuda")
+    wrong = wrong[(wrong < 0) | (wrong >= e)]
+    for renormalize in (True, False):
+        r = wb.route(z, k, renormalize=renormalize)
+        some = wrong[torch.arange(rows * k, device="cuda") % wrong.numel()].view(rows, k)
+        got = wb.route_backward(z, r._replace(experts=torch.where(away, some, r.experts)), d_gates, d_loss)
+        want = wb.route_backward(z, r._replace(experts=torch.where(away, torch.full_like(some, -1), r.experts)), d_gates, d_loss)
+        assert torch.equal(got, want), renormalize
