@@ -5,11 +5,14 @@
 // place of a result a call returns a text (what it refused) or the library's
 // negative status.
 #include <ATen/ATen.h>
+#include <c10/core/GradMode.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdint>
+#include <initializer_list>
 #include <stdexcept>
 #include <string>
+#include <utility>
 
 #include "../../include/wb.h"
 #include "args_ops.hpp"
@@ -52,6 +55,15 @@ const Tensor& needed(PyObject* o, const char* name, int64_t device) {
   const Tensor* t = tensor(o, name, device);
   if (!t) refuse(name, "is None");
   return *t;
+}
+
+// A result made here has no graph behind it: where one is being recorded, an
+// argument that requires a gradient would lose it without a word.
+void ungraded(std::initializer_list<std::pair<const Tensor*, const char*>> all) {
+  if (!c10::GradMode::is_enabled()) return;
+  for (const auto& [t, name] : all)
+    if (t && t->requires_grad())
+      refuse(name, "requires a gradient, which this operator does not have: detach it, or call under torch.no_grad()");
 }
 
 // [rows, cols], or [n, rows, cols] as its n * rows rows.
@@ -152,6 +164,7 @@ PyObject* wb_py_add_rms_norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const Tensor& x = needed(args[1], "x", at.device);
     const Tensor& weight = needed(args[2], "weight", at.device);
     const Tensor* residual = tensor(args[3], "residual", at.device);
+    ungraded({{&x, "x"}, {&weight, "weight"}, {residual, "residual"}});
     const wb_matrix mx = matrix(x, "x"), mw = vector(weight, "weight");
     const bool f8 = type == WB_F8E4M3;
     wb_matrix mr{}, mt{}, ms{};
@@ -230,6 +243,7 @@ PyObject* wb_py_route_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
     r.routed = plain(needed(args[8], "routed", at.device), at::kInt, 1, "routed").data_ptr<int32_t>();
     const Tensor* d_gates = tensor(args[9], "d_gates", at.device);
     const Tensor* d_loss = tensor(args[10], "d_loss", at.device);
+    ungraded({{d_gates, "d_gates"}, {d_loss, "d_loss"}});
     if (d_gates) plain(*d_gates, at::kFloat, count, "d_gates");
     if (d_loss) plain(*d_loss, at::kFloat, 1, "d_loss");
     Tensor d_logits = fresh(logits.sizes(), logits.scalar_type(), logits);
@@ -260,6 +274,8 @@ PyObject* wb_py_linear(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const Tensor* weight_scales = tensor(args[7], "weight_scales", at.device);
     const Tensor* bias = tensor(args[8], "bias", at.device);
     const Tensor* residual = tensor(args[9], "residual", at.device);
+    ungraded({{&x, "x"}, {&weight, "weight"}, {x_scales, "x_scales"}, {weight_scales, "weight_scales"}, {bias, "bias"},
+              {residual, "residual"}});
     wb_linear_args a{};
     a.x = matrix(x, "x"), a.weight = matrix(weight, "weight", offsets != nullptr);
     a.activation = static_cast<int32_t>(activation), a.gated = gated != 0;
@@ -317,6 +333,7 @@ PyObject* wb_py_combine(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const Tensor& gates = needed(args[3], "gates", at.device);
     const Tensor* residual = tensor(args[4], "residual", at.device);
     const Tensor* span = tensor(args[5], "span", at.device);
+    ungraded({{&y, "y"}, {&gates, "gates"}, {residual, "residual"}});
     const wb_matrix my = matrix(y, "y");
     if (positions.dim() != 2) refuse("positions", "does not have two dimensions");
     const int64_t rows = positions.size(0), k = positions.size(1);

@@ -9,7 +9,9 @@ float32, bfloat16 or float8_e4m3fn in the memory of the current device; rows
 may lie any distance apart. fp8 activations go with float32 scales of one row
 and 128 columns, [rows, ceil(cols / 128)]; fp8 weights with those of 128x128
 blocks, as unpacking writes them. Arguments that do not fit raise WbError.
-Only ``route`` has a gradient: the others serve a rollout rank's tensors.
+Only ``route`` has a gradient: the others serve a rollout rank's tensors, and
+raise WbError for one that requires a gradient while gradients are recorded (a
+differentiable ``route``'s gates go into ``combine`` detached).
 """
 
 from __future__ import annotations
@@ -114,7 +116,8 @@ def route(logits, k, mask=None, renormalize=True, stream=None):
 
 def route_backward(logits, routing, d_gates=None, d_loss=None, stream=None):
     """Gradient of ``logits`` from those of ``routing.gates`` [T, k] and
-    ``routing.loss`` (float32 tensors; None: zero), in the logits' type."""
+    ``routing.loss`` (float32 tensors; None: zero), in the logits' type. It has
+    no gradient in turn: d_gates and d_loss that require one raise WbError."""
     if stream is not None:
         return _on(stream, lambda: route_backward(logits, routing, d_gates, d_loss), logits, d_gates, d_loss,
                    *routing[:9])

@@ -626,3 +626,38 @@ def test_route_gradient_leaves_out_choices_that_are_no_experts(shape):
         got = wb.route_backward(z, r._replace(experts=torch.where(away, some, r.experts)), d_gates, d_loss)
         want = wb.route_backward(z, r._replace(experts=torch.where(away, torch.full_like(some, -1), r.experts)), d_gates, d_loss)
         assert torch.equal(got, want), renormalize
+
+
+# ---- operators without a gradient ---------------------------------------------------------------
+
+def test_operators_without_a_gradient_refuse_tensors_that_require_one():
+    """A result without a graph would lose the gradient silently."""
+    f = lambda *s: torch.ones(*s, dtype=torch.bfloat16, device="cuda")  # noqa: E731
+    need = lambda t: t.detach().clone().requires_grad_()  # noqa: E731
+    x, w, g, r, b = f(4, 64), f(32, 64), f(64), f(4, 64), f(32)
+    f8, xs, ws = torch.float8_e4m3fn, torch.ones(4, 1, device="cuda"), torch.ones(1, 1, device="cuda")
+    stacked, at = f(2, 32, 64), torch.tensor([0, 2, 4], dtype=torch.int32, device="cuda")
+    routing = wb.route(torch.randn(2, 8, device="cuda").requires_grad_(), 2)
+    assert routing.gates.requires_grad
+    z, plain = torch.randn(2, 8, device="cuda"), routing.gates.detach()
+    codes = lambda **k: wb.linear(x.to(f8), w.to(f8), **{"x_scales": xs, "weight_scales": ws, **k})  # noqa: E731
+    calls = [
+        lambda: wb.add_rms_norm(need(x), g), lambda: wb.add_rms_norm(x, need(g)), lambda: wb.add_rms_norm(x, g, need(r)),
+        lambda: wb.linear(need(x), w), lambda: wb.linear(x, need(w)), lambda: wb.linear(x, w, need(b)),
+        lambda: wb.linear(x, w, residual=need(f(4, 32))), lambda: codes(x_scales=need(xs)),
+        lambda: codes(weight_scales=need(ws)), lambda: wb.expert_linear(x, need(stacked), at),
+        lambda: wb.expert_linear(need(x), stacked, at), lambda: wb.combine(x, routing.positions, routing.gates),
+        lambda: wb.combine(need(x), routing.positions, plain),
+        lambda: wb.combine(x, routing.positions, plain, residual=need(f(2, 64))),
+        lambda: wb.route_backward(z, routing, need(plain)),
+        lambda: wb.route_backward(z, routing, plain, need(torch.ones((), device="cuda"))),
+    ]
+    for n, call in enumerate(calls):
+        with pytest.raises(wb.WbError, match="requires a gradient"):
+            call()
+        with torch.no_grad():
+            call()
+    # tensors that are part of no graph, and the router's own way back
+    wb.combine(x, routing.positions, routing.gates.detach())
+    wb.route_backward(need(z), routing, plain)
+    torch.cuda.synchronize()
