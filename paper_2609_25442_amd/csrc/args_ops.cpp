@@ -41,13 +41,15 @@ at::ScalarType type_of(int32_t code) {
   return code == WB_F32 ? at::kFloat : code == WB_BF16 ? at::kBFloat16 : at::kFloat8_e4m3fn;
 }
 
-// A tensor argument on the call's device; null for None.
+// A tensor argument on the call's device; null for None. One with a tangent of
+// forward-mode differentiation is refused: no result here would carry it on.
 const Tensor* tensor(PyObject* o, const char* name, int64_t device) {
   if (o == Py_None) return nullptr;
   if (!THPVariable_Check(o)) refuse(name, "is no tensor");
   const Tensor& t = THPVariable_Unpack(o);
   if (!t.defined() || !t.is_cuda() || t.layout() != at::kStrided) refuse(name, "is not in device memory");
   if (t.get_device() != device) refuse(name, "is on another device than the current one");
+  if (t._fw_grad(0).defined()) refuse(name, "has a forward-mode tangent, which the operators do not carry on");
   return &t;
 }
 

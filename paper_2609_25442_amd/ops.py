@@ -11,7 +11,8 @@ and 128 columns, [rows, ceil(cols / 128)]; fp8 weights with those of 128x128
 blocks, as unpacking writes them. Arguments that do not fit raise WbError.
 Only ``route`` has a gradient: the others serve a rollout rank's tensors, and
 raise WbError for one that requires a gradient while gradients are recorded (a
-differentiable ``route``'s gates go into ``combine`` detached).
+differentiable ``route``'s gates go into ``combine`` detached). Tensors with
+a forward-mode tangent are refused by all.
 """
 
 from __future__ import annotations
@@ -158,6 +159,10 @@ def _differentiable():
                 ctx.renormalize = renormalize
                 ctx.mark_non_differentiable(experts, positions, tokens, counts, offsets, routed)
                 return out
+
+            @staticmethod
+            def jvp(ctx, *_):
+                raise WbError(WB_EINVAL, "logits has a forward-mode tangent, which the operators do not carry on")
 
             @staticmethod
             @torch.autograd.function.once_differentiable

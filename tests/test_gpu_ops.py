@@ -661,3 +661,22 @@ def test_operators_without_a_gradient_refuse_tensors_that_require_one():
     wb.combine(x, routing.positions, routing.gates.detach())
     wb.route_backward(need(z), routing, plain)
     torch.cuda.synchronize()
+
+
+def test_operators_refuse_forward_mode_tangents():
+    import torch.autograd.forward_ad as fw
+
+    z, x, w, g = torch.randn(2, 8, device="cuda"), *(torch.ones(*s, dtype=torch.bfloat16, device="cuda") for s in ((2, 64), (32, 64), (64,)))
+    r = wb.route(z, 2)
+    with fw.dual_level():
+        dual = lambda t: fw.make_dual(t, torch.ones_like(t))  # noqa: E731
+        for n, call in enumerate([
+                lambda: wb.route(dual(z), 2), lambda: wb.route(dual(z.clone().requires_grad_()), 2),
+                lambda: wb.route_backward(dual(z), r, r.gates), lambda: wb.route_backward(z, r, dual(r.gates)),
+                lambda: wb.add_rms_norm(dual(x), g), lambda: wb.linear(x, dual(w)),
+                lambda: wb.combine(x, r.positions, dual(r.gates))]):
+            with pytest.raises(wb.WbError, match="tangent"):
+                call()
+        assert fw.unpack_dual(wb.route(z, 2).gates).tangent is None
+    wb.route(z, 2)
+    torch.cuda.synchronize()
