@@ -565,8 +565,9 @@ int wb_diff2_carry(const wb_field* fields, int32_t n, int32_t pass, int32_t last
  *     formulas have it; they stay in their rows.
  *   - fp8 is E4M3FN. Activations carry one fp32 scale per row and 128 columns,
  *     [rows, ceil(cols / 128)]: s = max |y| / 448 (1 if that is 0; NaN values
- *     are left out), q = E4M3(y / s). Weights carry one per 128 x 128 block,
- *     as wb_unpack writes them with quant_block 128.
+ *     are left out), q = E4M3(y / s), held to +-448 where s, below 2^-140, was
+ *     rounded down. Weights carry one per 128 x 128 block, as wb_unpack writes
+ *     them with quant_block 128.
  *   - An output must not overlap an input, except where a call says so. */
 typedef struct wb_matrix {
   void* data;

@@ -203,7 +203,9 @@ __device__ __forceinline__ RowScale row_scale(float amax) {
   return q;
 }
 
-// v / s rounded to fp32: one product, its remainder, one correction.
+// v / s rounded to fp32: one product, its remainder, one correction. A scale
+// among the smallest numbers can be rounded down by a third, so quotients of
+// such a one are held to what E4M3 has (a NaN stays one).
 template <int N>
 __device__ __forceinline__ void quotients(float (&v)[N], const RowScale& q) {
   if (q.near) {
@@ -212,7 +214,10 @@ __device__ __forceinline__ void quotients(float (&v)[N], const RowScale& q) {
       v[i] = __builtin_fmaf(__builtin_fmaf(-a, q.s, v[i]), q.r, a);
     }
   } else {
-    for (int i = 0; i < N; ++i) v[i] /= q.s;
+    for (int i = 0; i < N; ++i) {
+      v[i] /= q.s;
+      if (fabsf(v[i]) > 448.0f) v[i] = __builtin_copysignf(448.0f, v[i]);
+    }
   }
 }
 

@@ -680,3 +680,32 @@ def test_operators_refuse_forward_mode_tangents():
         assert fw.unpack_dual(wb.route(z, 2).gates).tangent is None
     wb.route(z, 2)
     torch.cuda.synchronize()
+
+
+# ---- fp8 results among the smallest numbers ------------------------------------------------------
+
+def test_fp8_results_of_subnormal_scales_are_no_nan():
+    """608 units of 2^-149 have a scale of 1.36 of them, one when rounded: their quotients are past E4M3's
+    largest, and are held to it."""
+    unit = 2.0 ** -149
+    w = torch.zeros(128, dtype=torch.float64)
+    w[:6] = torch.tensor([608.0, -608.0, 288.0, 97.0, -3.0, 1.0])
+    want = torch.tensor([448.0, -448.0, 288.0, 96.0, -3.0, 1.0])
+    x = torch.ones(3, 128, device="cuda")
+    x[1, 7] = math.nan
+    q, s, _ = wb.add_rms_norm(x, (w * unit).float().cuda(), eps=0.0, out_dtype="f8e4m3")
+    for t in (0, 2):  # y is the weight itself
+        assert float(s[t, 0]) == unit and torch.equal(q[t].float().cpu()[:6], want), q[t, :6].float()
+        assert torch.all(q[t, 6:].float() == 0)
+    assert torch.isnan(q[1].float()).all()
+    # the same as sums of two products of codes, few rows and many
+    f8 = torch.float8_e4m3fn
+    codes = torch.zeros(256, 128)
+    codes[:6, :2] = torch.tensor([[448.0, 160.0], [-448.0, -160.0], [288.0, 0.0], [96.0, 1.0], [-3.0, 0.0], [1.0, 0.0]])
+    for rows in (1, 700, 9000):
+        a = torch.zeros(rows, 128)
+        a[:, :2] = 1.0
+        got, gs = wb.linear(a.to(f8).cuda(), codes.to(f8).cuda(), x_scales=torch.full((rows, 1), 2.0 ** -75, device="cuda"),
+                            weight_scales=torch.full((2, 1), 2.0 ** -74, device="cuda"), out_dtype="f8e4m3")
+        assert torch.all(gs[:, 0] == unit) and torch.all(gs[:, 1] == 1.0), rows
+        assert torch.equal(got[:, :6].float().cpu(), want.expand(rows, 6)) and torch.all(got[:, 6:].float() == 0), rows
