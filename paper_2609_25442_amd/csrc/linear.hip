@@ -700,6 +700,13 @@ int64_t row_tiles(const LinearArgs& a, int per) {
   return std::min<int64_t>(a.rows, a.rows / per + std::min<int64_t>(a.num_experts, a.rows));
 }
 
+int64_t col_tiles(const LinearArgs& a, int bn) {
+  const int step = a.gated ? bn / 2 : bn;
+  return (a.n_out + step - 1) / step;
+}
+
+constexpr int64_t kMaxTiles = 0x3fffff;  // of a launch: up to 512 threads each, 2^32 in all
+
 template <class S, bool F8, bool DIRECT>
 hipError_t launch_tile(const LinearArgs& a, hipStream_t st) {
   const auto kernel = wb_linear_tile_kernel<S, F8, DIRECT>;
@@ -714,10 +721,7 @@ hipError_t launch_tile(const LinearArgs& a, hipStream_t st) {
     if (e != hipSuccess) return e;
     raised.fetch_or(bit, std::memory_order_release);
   }
-  const int step = a.gated ? S::BN / 2 : S::BN;
-  const int64_t tiles_n = (a.n_out + step - 1) / step;
-  const int64_t all = row_tiles(a, S::BM) * tiles_n;
-  if (all > 0x3fffff) return hipErrorInvalidConfiguration;
+  const int64_t tiles_n = col_tiles(a, S::BN), all = row_tiles(a, S::BM) * tiles_n;
   hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>(all)), dim3(S::kThreads), S::kLds, st, a,
                      static_cast<uint32_t>(tiles_n), 8u);
   return hipGetLastError();
@@ -757,6 +761,8 @@ bool holds_scales(const LinearArgs& a, int choice) {
   return (a.gated ? kChoices[choice].bn / 2 : kChoices[choice].bn) % kScaleBlock == 0;
 }
 
+// The tile, and the us that it is expected to take; -1 where one launch takes
+// the tiles of no shape.
 int choose(const LinearArgs& a, double* expected) {
   const int f8 = a.in_type == WB_F8E4M3;
   const double stages = std::ceil(double(a.k) * (f8 ? 1 : 2) / kStageBytes);
@@ -765,11 +771,12 @@ int choose(const LinearArgs& a, double* expected) {
   for (int i = 0; i < kNumChoices; ++i) {
     const Choice& c = kChoices[i];
     if (!a.direct && c.by_registers[f8] == 0.0f) continue;
-    const int step = a.gated ? c.bn / 2 : c.bn;
+    const int64_t tiles_n = col_tiles(a, c.bn);
+    if (row_tiles(a, c.bm) * tiles_n > kMaxTiles) continue;
     // of the experts' last tiles about half are empty
     double tiles_m = double(row_tiles(a, c.bm));
     if (a.offsets) tiles_m = std::min(double(a.rows), double(a.rows) / c.bm + 0.5 * std::min<int64_t>(a.num_experts, a.rows));
-    const double tiles = tiles_m * ((a.n_out + step - 1) / step);
+    const double tiles = tiles_m * double(tiles_n);
     // a residual is read between the products and the stores, at about the
     // stores' cost; what is left of 256 tiles or fewer has the CUs to itself
     const int more = a.residual ? 2 : 1;
@@ -818,11 +825,11 @@ Form form_of(const LinearArgs& a) {
     if (b.direct && x_rows <= most / (pitch / 16) && w_rows <= most / (pitch / 16)) {
       const int choice = choose(b, &copied_us);
       copied_us += kCopyUs + double(x_rows + w_rows) * pitch / kCopyBytesPerUs;
-      if (copied_us < us)
+      if (choice >= 0 && (f.choice < 0 || copied_us < us))
         f.a = b, f.choice = choice, f.copy_x = x, f.copy_weight = weight, f.x_bytes = x_rows * pitch, f.weight_bytes = w_rows * pitch;
     }
   }
-  if (a.out_type == WB_F8E4M3 && !holds_scales(a, f.choice)) f.sums_bytes = static_cast<size_t>(a.rows) * a.n_out * sizeof(float);
+  if (a.out_type == WB_F8E4M3 && f.choice >= 0 && !holds_scales(a, f.choice)) f.sums_bytes = static_cast<size_t>(a.rows) * a.n_out * sizeof(float);
   return f;
 }
 
@@ -863,9 +870,10 @@ bool linear_near(const LinearArgs& a) {
          !(a.in_type == WB_F8E4M3 && a.gated && a.n_out % 16 != 0);
 }
 
-size_t linear_workspace_bytes(const LinearArgs& a) {
+int64_t linear_workspace_bytes(const LinearArgs& a) {
   if (a.rows == 0) return 0;
   const Form f = form_of(a);
+  if (f.choice < 0) return -1;
   return f.x_bytes + f.weight_bytes + f.sums_bytes;
 }
 

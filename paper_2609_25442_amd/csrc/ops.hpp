@@ -96,7 +96,7 @@ struct LinearArgs {
 };
 
 size_t route_workspace_bytes(int64_t rows, int32_t experts);
-size_t linear_workspace_bytes(const LinearArgs& a);
+int64_t linear_workspace_bytes(const LinearArgs& a);  // -1: more tiles than one launch takes, nothing to launch
 
 // Whether 32-bit offsets reach the rows of x and weight, and sixteen rows of
 // the weight share a scale.

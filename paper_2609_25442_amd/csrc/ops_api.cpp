@@ -93,6 +93,8 @@ int too_many_rows(int64_t rows) {
 
 int launched(int e, const char* what) { return e == 0 ? WB_OK : hip_fail(static_cast<hipError_t>(e), what); }
 
+int too_many_tiles() { return set_error(WB_EUNSUPPORTED, "more tiles than one launch takes"); }
+
 int check_route(const wb_matrix* logits, const uint8_t* mask, int32_t k, Operands& ops) {
   if (!logits) return set_error(WB_EINVAL, "null argument");
   const int rc = too_many_rows(logits->rows);
@@ -289,7 +291,9 @@ int wb_linear_workspace(const wb_linear_args* p, size_t* bytes) {
     wb::LinearArgs a{};
     const int rc = check_linear(p, ops, a, false);
     if (rc != WB_OK) return rc;
-    *bytes = wb::linear_workspace_bytes(a);
+    const int64_t need = wb::linear_workspace_bytes(a);
+    if (need < 0) return too_many_tiles();
+    *bytes = static_cast<size_t>(need);
     return WB_OK;
   });
 }
@@ -300,14 +304,12 @@ int wb_linear(const wb_linear_args* p, void* workspace, size_t workspace_bytes, 
     wb::LinearArgs a{};
     const int rc = check_linear(p, ops, a, true);
     if (rc != WB_OK) return rc;
-    const size_t need = wb::linear_workspace_bytes(a);
-    if (workspace_bytes < need) return set_error(WB_ESIZE, "workspace smaller than wb_linear_workspace");
-    if (need)
-      ops.rc = check_extent_as(workspace, static_cast<int64_t>(need), [] { return std::string("workspace"); }, 16, &ops.range);
+    const int64_t need = wb::linear_workspace_bytes(a);
+    if (need < 0) return too_many_tiles();
+    if (workspace_bytes < static_cast<size_t>(need)) return set_error(WB_ESIZE, "workspace smaller than wb_linear_workspace");
+    if (need) ops.rc = check_extent_as(workspace, need, [] { return std::string("workspace"); }, 16, &ops.range);
     if (ops.rc != WB_OK) return ops.rc;
-    const int launch = wb::launch_linear(a, workspace, stream);
-    if (launch == hipErrorInvalidConfiguration) return set_error(WB_EUNSUPPORTED, "more tiles than one launch takes");
-    return launched(launch, "product launch");
+    return launched(wb::launch_linear(a, workspace, stream), "product launch");
   });
 }
 

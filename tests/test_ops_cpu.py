@@ -136,3 +136,20 @@ def test_operators_refuse_cpu_tensors():
         wb.linear(x, x, activation="tanh")
     with pytest.raises(wb.WbError):
         wb.expert_linear(x, x, None)
+
+
+def test_linear_takes_tiles_that_one_launch_can():
+    """128 x 128 tiles would be expected to end first, but are 8.7 million; of 256 x 256 there are 2.2 million, and
+    their 128 columns hold the scales of a gated result, so that no fp32 rows are asked for."""
+    rows, n = 4194303, 34000
+    a = linear(x=m(rows, 64), weight=m(n, 64), out=m(rows, n // 2, F8), out_scales=m(rows, 133, F32), gated=1)
+    assert workspace(a) == (wb.WB_OK, 0)
+
+
+def test_linear_refuses_more_tiles_than_a_launch_takes():
+    """Before anything is launched, and with every size within its own limit."""
+    rows, n = 4194303, 1 << 26
+    for k in (64, 63):  # rows on the 16-byte grid, and rows that would be copied onto it first
+        a = linear(x=m(rows, k), weight=m(n, k), out=m(rows, n))
+        assert workspace(a)[0] == wb.WB_EUNSUPPORTED
+        assert b"tiles" in wb.lib.wb_last_error()
