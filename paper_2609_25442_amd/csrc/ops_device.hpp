@@ -174,6 +174,15 @@ __device__ __forceinline__ float sum_of_wave(float v) {
   return v;
 }
 
+// exp(x) of x <= 0, to within two roundings: 2^(x log2 e), the product's
+// remainder and the constant's put back in.
+__device__ __forceinline__ float exp_below(float x) {
+  x = x < -150.0f ? -150.0f : x;  // 0; NaN stays
+  const float hi = x * 1.44269502f, lo = __builtin_fmaf(x, 1.92596299e-8f, __builtin_fmaf(x, 1.44269502f, -hi));
+  const float e = __builtin_amdgcn_exp2f(hi);
+  return __builtin_fmaf(e * lo, 0.693147182f, e);
+}
+
 struct Sum {
   __device__ __forceinline__ float operator()(float a, float b) const { return a + b; }
 };

@@ -109,15 +109,6 @@ __device__ __forceinline__ void load_logits(const void* base, int64_t row, int64
   }
 }
 
-// exp(x) of x <= 0, to within two roundings: 2^(x log2 e), the product's
-// remainder and the constant's put back in.
-__device__ __forceinline__ float exp_below(float x) {
-  x = x < -150.0f ? -150.0f : x;  // 0; NaN stays
-  const float hi = x * 1.44269502f, lo = __builtin_fmaf(x, 1.92596299e-8f, __builtin_fmaf(x, 1.44269502f, -hi));
-  const float e = __builtin_amdgcn_exp2f(hi);
-  return __builtin_fmaf(e * lo, 0.693147182f, e);
-}
-
 // exp(z - top) of a row, one over the sum, and whether the row has a logit
 // above -inf. A NaN or +inf logit makes the sum NaN.
 template <class W>

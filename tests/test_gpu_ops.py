@@ -709,3 +709,34 @@ def test_fp8_results_of_subnormal_scales_are_no_nan():
                             weight_scales=torch.full((2, 1), 2.0 ** -74, device="cuda"), out_dtype="f8e4m3")
         assert torch.all(gs[:, 0] == unit) and torch.all(gs[:, 1] == 1.0), rows
         assert torch.equal(got[:, :6].float().cpu(), want.expand(rows, 6)) and torch.all(got[:, 6:].float() == 0), rows
+
+
+# ---- roundings of the activations and of the router ----------------------------------------------
+
+@pytest.mark.parametrize("k", [1, 16], ids=["registers", "direct"])
+def test_silu_is_within_a_few_roundings(k):
+    """z itself is exact (one product by one). Roundings of half a unit: e^-|z| three (the instruction's unit and a
+    sum), 1 + t one and at most half of the three, its reciprocal one, z t one more, their product one: nine."""
+    z = torch.cat([torch.linspace(-85, 88, 4001), torch.logspace(-30, 1.9, 2001), -torch.logspace(-30, 1.9, 2001)]).bfloat16()
+    w, x = torch.zeros(z.numel(), k, dtype=torch.bfloat16), torch.zeros(2, k, dtype=torch.bfloat16)
+    w[:, 0], x[:, 0] = z, 1.0
+    got = wb.linear(gpu(x), gpu(w), activation="silu", out_dtype="f32").double().cpu()
+    want = z.double() * torch.sigmoid(z.double())
+    off = ((got - want).abs() - 9 * ref.U32 * want.abs()).amax(0)
+    assert float(off.max()) <= 0, (float(z[off.argmax()]), float((got - want).abs().amax(0)[off.argmax()] / want.abs()[off.argmax()] / ref.U32))
+    # gated, by an up of one
+    both = torch.cat([w, w])
+    both[z.numel():, 0] = 1.0
+    assert torch.equal(wb.linear(gpu(x), gpu(both), activation="silu", gated=True, out_dtype="f32").double().cpu(), got)
+
+
+def test_silu_of_the_ends():
+    z = torch.tensor([0.0, -0.0, 100.0, 3e38, math.inf, -100.0, -200.0, -3e38, math.nan]).bfloat16()
+    w = torch.zeros(z.numel(), 16, dtype=torch.bfloat16)
+    w[:, 0] = z
+    x = torch.zeros(1, 16, dtype=torch.bfloat16)
+    x[0, 0] = 1.0
+    w[4, 1:], w[8, 1:] = 0.0, 0.0
+    got = wb.linear(gpu(x), gpu(w), activation="silu", out_dtype="f32")[0].cpu()
+    assert torch.equal(got[:2], torch.zeros(2)) and torch.equal(got[2:5], z[2:5].float())
+    assert torch.all(got[5:8].abs() <= 1e-38) and torch.isnan(got[8])
