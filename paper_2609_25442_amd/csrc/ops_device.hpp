@@ -174,13 +174,14 @@ __device__ __forceinline__ float sum_of_wave(float v) {
   return v;
 }
 
-// exp(x) of x <= 0, to within two roundings: 2^(x log2 e), the product's
-// remainder and the constant's put back in.
+// exp(x) of x <= 0 as 2^n 2^f, x log2 e = n + f with the constant in two parts:
+// f is off by a rounding of a number of at most a half, so that the
+// instruction's unit is nearly all that the result is off by.
 __device__ __forceinline__ float exp_below(float x) {
   x = x < -150.0f ? -150.0f : x;  // 0; NaN stays
-  const float hi = x * 1.44269502f, lo = __builtin_fmaf(x, 1.92596299e-8f, __builtin_fmaf(x, 1.44269502f, -hi));
-  const float e = __builtin_amdgcn_exp2f(hi);
-  return __builtin_fmaf(e * lo, 0.693147182f, e);
+  const float n = __builtin_rintf(x * 1.44269502f);
+  const float f = __builtin_fmaf(x, 1.92596299e-8f, __builtin_fmaf(x, 1.44269502f, -n));
+  return __builtin_ldexpf(__builtin_amdgcn_exp2f(f), static_cast<int>(n));
 }
 
 struct Sum {

@@ -109,22 +109,28 @@ __device__ __forceinline__ void load_logits(const void* base, int64_t row, int64
   }
 }
 
-// exp(z - top) of a row, one over the sum, and whether the row has a logit
-// above -inf. A NaN or +inf logit makes the sum NaN.
+// The sum of a lane's registers, by halves: as many roundings on the way of
+// each as there are halvings.
+template <int N>
+__device__ __forceinline__ float sum_of(const float* v) {
+  if constexpr (N == 1)
+    return v[0];
+  else
+    return sum_of<N / 2>(v) + sum_of<N / 2>(v + N / 2);
+}
+
+// exp(z - top) of a row, their sum, one over it, and whether the row has a
+// logit above -inf. A NaN or +inf logit makes the sum NaN.
 template <class W>
-__device__ __forceinline__ bool softmax_row(const float (&z)[W::R], float (&e)[W::R], float& r, float& top) {
+__device__ __forceinline__ bool softmax_row(const float (&z)[W::R], float (&e)[W::R], float& sum, float& r, float& top) {
   top = -__builtin_inff();
 #pragma unroll
   for (int j = 0; j < W::R; ++j) top = fmaxf(top, z[j]);
   top = W::reduce(top, FMax());
   if (top == -__builtin_inff()) top = 0.0f;
-  float sum = 0.0f;
 #pragma unroll
-  for (int j = 0; j < W::R; ++j) {
-    e[j] = exp_below(z[j] - top);
-    sum += e[j];
-  }
-  sum = W::reduce(sum, Sum());
+  for (int j = 0; j < W::R; ++j) e[j] = exp_below(z[j] - top);
+  sum = W::reduce(sum_of<W::R>(e), Sum());
   r = 1.0f / sum;
   return sum != 0.0f;
 }
@@ -150,10 +156,10 @@ __device__ void route_block(const RouteArgs& a, const Partials& part, int64_t bl
   for (int j = 0; j < R; ++j) acc[j] = 0.0f;
   const int64_t end = min(a.rows, (block + 1) * per);
   for (int64_t row = block * per + group; row < end; row += T / L) {
-    float z[R], e[R], r, top;
+    float z[R], e[R], sum, r, top;
     const bool masked = a.mask && !a.mask[row];
     load_logits<W>(a.logits, row, a.ld_logits, a.logits_type, a.num_experts, l, z);
-    const bool routed = softmax_row<W>(z, e, r, top) && !masked;
+    const bool routed = softmax_row<W>(z, e, sum, r, top) && !masked;
     if (routed) {
 #pragma unroll
       for (int j = 0; j < R; ++j) acc[j] = __builtin_fmaf(e[j], r, acc[j]);
@@ -163,7 +169,7 @@ __device__ void route_block(const RouteArgs& a, const Partials& part, int64_t bl
     // lane that had it needs its next, which all the lanes of the row look for
     // in the row's copy in LDS: a third of the instructions of a pass over
     // every lane's registers, where those are many.
-    float lane_best = -__builtin_inff(), chosen = 0.0f;
+    float lane_best = -__builtin_inff();
     int lane_at = W::E;
     float* const mine = s_row + group * (L * kPitch);
     if constexpr (kShared) {
@@ -208,20 +214,22 @@ __device__ void route_block(const RouteArgs& a, const Partials& part, int64_t bl
       float g = exp_below(best - top) + (r - r);  // NaN where the row's sum is
       const bool none = !routed || best == -__builtin_inff();
       if (none) at = -1, g = 0.0f;
-      chosen += g;
       if (l == 0) {
         s_gate[group][i] = g;
         s_expert[group][i] = at;
         if (!none) atomicAdd(&s_count[at], 1);
       }
     }
-    // over the sum of the chosen, or of all
-    const float scale = a.renormalize ? 1.0f / chosen : r;
     order_lanes();
+    // over the sum of the chosen, or of all
+    float over = 0.0f;
+    for (int i = l; i < a.k; i += L) over += s_gate[group][i];
+    over = W::reduce(over, Sum());
+    if (!a.renormalize) over = sum;
     for (int i = l; i < a.k; i += L) {
       const int at = s_expert[group][i];
       a.experts[row * a.k + i] = at;
-      a.gates[row * a.k + i] = at < 0 ? 0.0f : s_gate[group][i] * scale;
+      a.gates[row * a.k + i] = at < 0 ? 0.0f : s_gate[group][i] / over;
     }
     order_lanes();
   }
@@ -415,7 +423,7 @@ __global__ __launch_bounds__(kGradThreads) void wb_route_grad_kernel(RouteGradAr
     of_loss[j] = W::expert(l, j) < a.num_experts ? scale * static_cast<float>(a.counts[W::expert(l, j)]) : 0.0f;
   const int64_t stride = int64_t(gridDim.x) * kGroups;
   for (int64_t row = int64_t(blockIdx.x) * kGroups + group; row < a.rows; row += stride) {
-    float z[R], p[R], d[R], r, top;
+    float z[R], p[R], d[R], sum, r, top;
     // the lane's first choice, on its way with the logits
     struct {
       int32_t expert;
@@ -425,12 +433,16 @@ __global__ __launch_bounds__(kGradThreads) void wb_route_grad_kernel(RouteGradAr
     if (a.d_gates && l < a.k) first = {a.experts[row * a.k + l], a.gates[row * a.k + l], a.d_gates[row * a.k + l]};
     const bool masked = a.mask && !a.mask[row];
     load_logits<W>(a.logits, row, a.ld_logits, a.logits_type, a.num_experts, l, z);
-    const bool routed = softmax_row<W>(z, p, r, top) && !masked;
+    const bool routed = softmax_row<W>(z, p, sum, r, top) && !masked;
     const int32_t* experts = a.experts + row * a.k;
     const float* gates = a.gates + row * a.k;
     const float* d_gates = a.d_gates ? a.d_gates + row * a.k : nullptr;
 #pragma unroll
-    for (int j = 0; j < R; ++j) p[j] *= r, d[j] = of_loss[j];
+    for (int j = 0; j < R; ++j) {
+      const float q = p[j] * r;  // p / sum: the product, its remainder, one correction
+      p[j] = __builtin_fmaf(__builtin_fmaf(-q, sum, p[j]), r, q);
+      d[j] = of_loss[j];
+    }
     if (d_gates && !a.renormalize) {
 #pragma unroll
       for (int j = 0; j < R; ++j) mine[W::expert(l, j)] = d[j];
@@ -442,12 +454,12 @@ __global__ __launch_bounds__(kGradThreads) void wb_route_grad_kernel(RouteGradAr
 #pragma unroll
       for (int j = 0; j < R; ++j) d[j] = mine[W::expert(l, j)];
     }
-    float mean = 0.0f;
+    float mean[4] = {0, 0, 0, 0};
 #pragma unroll
-    for (int j = 0; j < R; ++j) mean = __builtin_fmaf(p[j], d[j], mean);
-    mean = W::reduce(mean, Sum());
+    for (int j = 0; j < R; ++j) mean[j & 3] = __builtin_fmaf(p[j], d[j], mean[j & 3]);
+    const float of_all = W::reduce(sum_of<4>(mean), Sum());
 #pragma unroll
-    for (int j = 0; j < R; ++j) d[j] = p[j] * (d[j] - mean);
+    for (int j = 0; j < R; ++j) d[j] = p[j] * (d[j] - of_all);
     if (d_gates && a.renormalize) {
 #pragma unroll
       for (int j = 0; j < R; ++j) mine[W::expert(l, j)] = d[j];

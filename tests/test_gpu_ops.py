@@ -740,3 +740,39 @@ def test_silu_of_the_ends():
     got = wb.linear(gpu(x), gpu(w), activation="silu", out_dtype="f32")[0].cpu()
     assert torch.equal(got[:2], torch.zeros(2)) and torch.equal(got[2:5], z[2:5].float())
     assert torch.all(got[5:8].abs() <= 1e-38) and torch.isnan(got[8])
+
+
+@pytest.mark.parametrize("experts,k", [(8, 2), (8, 8), (64, 6), (256, 8), (1024, 8)])
+@pytest.mark.parametrize("renormalize", [True, False])
+def test_gates_and_gradient_are_off_by_no_more_than_the_formula_in_fp32(experts, k, renormalize):
+    """A gate takes the roundings of an exponential, of a sum and of a quotient, as elementary operations in fp32 do:
+    their root mean squares over 20000 rows are the same but for 0.5 % of spread in each, 3 % being four of both."""
+    say("roundings", experts, k, renormalize)
+    g = torch.Generator(device="cuda").manual_seed(experts + k)
+    rows = 20000
+    z = torch.randn(rows, experts, generator=g, device="cuda") * 1.5
+    d_gates, d_loss = torch.randn(rows, k, generator=g, device="cuda"), torch.tensor(0.7 * rows, device="cuda")
+    r = wb.route(z, k, renormalize=renormalize)
+    at = r.experts.long()
+
+    def formula(z, type):
+        top = z.amax(1, keepdim=True)
+        e = torch.exp(z - top)
+        p = e / e.sum(1, keepdim=True)
+        gates = e.gather(1, at)
+        gates = gates / (gates if renormalize else e).sum(1, keepdim=True)
+        dg = d_gates.to(type)
+        dp = (r.counts.to(type) * (experts / (k * rows * rows)) * d_loss.to(type)).expand(rows, experts)
+        if not renormalize:
+            dp = dp.scatter_add(1, at, dg)
+        d = p * (dp - (p * dp).sum(1, keepdim=True))
+        if renormalize:
+            d = d.scatter_add(1, at, gates * (dg - (dg * gates).sum(1, keepdim=True)))
+        return gates, d
+
+    want, plain = formula(z.double(), torch.float64), formula(z, torch.float32)
+    got = r.gates, wb.route_backward(z, r, d_gates, d_loss)
+    rms = lambda a, w: float(((a.double() - w) / w).square().mean().sqrt())  # noqa: E731
+    assert rms(got[0], want[0]) <= 1.03 * rms(plain[0], want[0]), "gates"
+    off = lambda a: float((a.double() - want[1]).norm())  # noqa: E731
+    assert off(got[1]) <= 1.03 * off(plain[1]), "gradient"
