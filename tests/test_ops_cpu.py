@@ -2,9 +2,11 @@
 sizes they ask for, without a GPU."""
 
 import ctypes
+import math
 
 import pytest
 
+import ops_tiles as tiles
 import paper_2609_25442_amd as wb
 
 F32, BF16, F8 = 0, 1, 2
@@ -153,3 +155,66 @@ def test_linear_refuses_more_tiles_than_a_launch_takes():
         a = linear(x=m(rows, k), weight=m(n, k), out=m(rows, n))
         assert workspace(a)[0] == wb.WB_EUNSUPPORTED
         assert b"tiles" in wb.lib.wb_last_error()
+
+
+def product(rows, n, k, f8, gated=False, experts=0, residual=False, out="bf16", x_rows=None):
+    """The C call's arguments of contiguous operands."""
+    t, cols, xr = F8 if f8 else BF16, n // 2 if gated else n, rows if x_rows is None else x_rows
+    nb = lambda c: -(-c // 128)  # noqa: E731
+    a = Args()
+    a.x, a.weight, a.gated = m(xr, k, t), m(n * max(1, experts), k, t), int(gated)
+    if f8:
+        a.x_scales, a.weight_scales = m(xr, nb(k), F32), m(nb(n) * max(1, experts), nb(k), F32)
+    if experts:
+        a.num_experts, a.offsets = experts, 4096
+        a.tokens = 4096 if x_rows is not None else None
+    if residual:
+        a.residual = m(rows, cols)
+    a.out = m(rows, cols, {"bf16": BF16, "f32": F32, "f8e4m3": F8}[out])
+    if out == "f8e4m3":
+        a.out_scales = m(rows, nb(cols), F32)
+    return a
+
+
+def test_workspaces_are_those_of_the_tiles_the_rule_takes():
+    """The copies of the operands and the fp32 rows of fp8 results depend on the tile: the rule written out in
+    ops_tiles gives the library's bytes exactly."""
+    import random
+
+    rng = random.Random(3)
+    size = lambda lo, hi: int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))  # noqa: E731
+    seen = set()
+    for _ in range(4000):
+        rows, n, k = size(1, 16384), 2 * size(8, 8192), size(16, 8192)
+        if rng.random() < 0.6:
+            rows, n, k = (max(1, rows // 64 * 64), max(64, n // 64 * 64), max(16, k // 16 * 16))
+        more = dict(gated=rng.random() < 0.5, residual=rng.random() < 0.3, out=rng.choice(["bf16", "f32", "f8e4m3", "f8e4m3"]),
+                    experts=rng.choice([0, 0, 1, 8, 40]))
+        if more["experts"] and rng.random() < 0.5:
+            more["x_rows"] = max(1, rows // 4)
+        f8 = rng.random() < 0.5
+        tile, way, need = tiles.form(rows, n, k, f8, **more)
+        assert workspace(product(rows, n, k, f8, **more)) == (wb.WB_OK, need), (rows, n, k, f8, more, tile, way)
+        seen.add((tile, way))
+    assert len(seen) > 20
+
+
+def test_linear_workspace_of_fp8_results_is_the_tile_s():
+    # 16 x 32 tiles hold no scale's columns; 128 x 128 do, and 256 x 256 those of a gated result
+    assert workspace(product(4, 4096, 4096, False, out="f8e4m3")) == (wb.WB_OK, 4 * 4096 * 4)
+    assert workspace(product(4, 4096, 64, False, out="f8e4m3")) == (wb.WB_OK, 0)  # one step: 128 x 128 ends before two launches
+    assert workspace(product(1024, 8192, 1024, True, out="f8e4m3")) == (wb.WB_OK, 0)
+    assert workspace(product(8192, 8192, 1024, False, gated=True, out="f8e4m3")) == (wb.WB_OK, 0)
+    assert workspace(product(128, 4096, 7168, True, gated=True, experts=32, x_rows=32, out="f8e4m3")) == (wb.WB_OK, 128 * 2048 * 4)
+
+
+def test_sizes_of_the_products_tests_take_every_tile():
+    """Each tile in each type and way that the table has, plain and stacked, plain and gated."""
+    want = {(t, f8, "direct") for t in range(len(tiles.TABLE)) for f8 in (False, True)}
+    want |= {(t, f8, "registers") for t, c in enumerate(tiles.TABLE) for f8 in (False, True) if c["by_registers"][f8]}
+    assert set(tiles.SIZES) == want
+    for (tile, f8, way), sizes in tiles.SIZES.items():
+        for s in sizes:
+            assert tiles.form_of_size(f8, s)[:2] == (tile, way), (tile, f8, way, s)
+        assert {bool(s[4]) for s in sizes} == {False, True}, (tile, f8, way)
+        assert {tiles.FORMS[s[0]].get("gated", False) for s in sizes} == {False, True}, (tile, f8, way)
