@@ -776,3 +776,63 @@ def test_gates_and_gradient_are_off_by_no_more_than_the_formula_in_fp32(experts,
     assert rms(got[0], want[0]) <= 1.03 * rms(plain[0], want[0]), "gates"
     off = lambda a: float((a.double() - want[1]).norm())  # noqa: E731
     assert off(got[1]) <= 1.03 * off(plain[1]), "gradient"
+
+
+# ---- rows that 32-bit offsets do not reach --------------------------------------------------------
+
+def far(t, apart):
+    """The same values with rows ``apart`` elements from each other, in memory that is otherwise left as it is."""
+    rows, cols = t.shape
+    view = torch.empty((rows - 1) * apart + cols, dtype=t.dtype, device="cuda").as_strided((rows, cols), (apart, 1))
+    view.copy_(gpu(t))
+    return view
+
+
+@pytest.mark.parametrize("f8", [False, True], ids=["bf16", "f8"])
+@pytest.mark.parametrize("which", ["x", "weight", "gathered x"])
+def test_products_of_rows_far_apart(which, f8):
+    """Past 2^32 bytes from the first row to the last: the offsets in registers are 32 bits wide."""
+    say("linear far", which, f8)
+    apart = (1 << 24) // (1 if f8 else 2)  # 16 MiB
+    x, w, xs, ws, b, r, cols = product_inputs(300, 288, 208, f8, FORMS[2])
+    gx, gw = (gpu(x), far(w[0], apart)) if which == "weight" else (far(x, apart), gpu(w[0]))
+    more = dict(x_scales=gpu(xs), weight_scales=gpu(ws and ws[0]), activation="gelu", residual=gpu(r), out_dtype="f32")
+    if which == "gathered x":
+        tokens = (torch.arange(300, dtype=torch.int32) * 7 + 290) % 300
+        at = torch.tensor([0, 300], dtype=torch.int32, device="cuda")
+        got = wb.expert_linear(gx, gw[None], at, gpu(tokens), gpu(b[0])[None], **{**more, "weight_scales": ws and gpu(ws[0])[None]})
+        x, xs = x[tokens.long()], None if xs is None else xs[tokens.long()]
+    else:
+        got = wb.linear(gx, gw, gpu(b[0]), **more)
+    want, err = ref.product(x, w[0], b[0], "gelu", False, r, xs, ws and ws[0])
+    ref.check(got, want, err, which)
+
+
+def test_stacked_weights_past_four_gigabytes():
+    """Each expert's rows start past 32 bits from the first expert's; within an expert they are near."""
+    say("experts far")
+    apart, n, k, e = 1 << 21, 96, 128, 25  # 4 MiB a row, 9.4 GiB in all
+    w = ref.randn(n * e, k, seed=3, dtype="bf16", scale=k ** -0.5)
+    x = ref.randn(2 * e, k, seed=4, dtype="bf16")
+    stacked = far(w, apart).unflatten(0, (e, n))
+    at = torch.arange(0, 2 * e + 1, 2, dtype=torch.int32)
+    got = wb.expert_linear(gpu(x), stacked, gpu(at), out_dtype="f32")
+    parts = [ref.product(x[2 * i:2 * i + 2], w[n * i:n * i + n], None, "none", False, None) for i in range(e)]
+    ref.check(got, torch.cat([p[0] for p in parts]), torch.cat([p[1] for p in parts]), "experts")
+
+
+def test_norm_sum_and_routing_of_rows_far_apart():
+    say("rows far")
+    apart = 1 << 22
+    x, r, w = ref.randn(600, 300, seed=1, dtype="f32"), ref.randn(600, 300, seed=2, dtype="bf16"), ref.randn(300, seed=3)
+    for out in ("bf16", "f8e4m3"):
+        got = wb.add_rms_norm(far(x, apart), gpu(w), far(r, apart), out_dtype=out)
+        want = wb.add_rms_norm(gpu(x), gpu(w), gpu(r), out_dtype=out)
+        assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(got, want) if a is not None)
+    pos = torch.randperm(1200, generator=torch.Generator().manual_seed(1)).view(600, 2).int() % 600
+    gates = ref.randn(600, 2, seed=5)
+    assert torch.equal(wb.combine(far(x, apart), gpu(pos), gpu(gates), residual=far(r, apart)),
+                       wb.combine(gpu(x), gpu(pos), gpu(gates), residual=gpu(r)))
+    a, b = wb.route(far(x, apart), 6), wb.route(gpu(x), 6)
+    assert all(torch.equal(u, v) for u, v in zip(a[:8], b[:8]))
+    assert torch.equal(wb.route_backward(far(x, apart), a, torch.ones_like(a.gates)), wb.route_backward(gpu(x), b, torch.ones_like(b.gates)))
