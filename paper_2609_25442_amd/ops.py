@@ -20,7 +20,7 @@ from __future__ import annotations
 import collections
 import ctypes
 
-from . import DTYPES, WB_EINVAL, WbError, _args, lib
+from . import DTYPES, WB_EINVAL, WB_EUNSUPPORTED, WbError, _args, lib
 
 ACTIVATIONS = {"none": 0, "silu": 1, "gelu": 2}
 _torch = None
@@ -107,7 +107,7 @@ def route(logits, k, mask=None, renormalize=True, stream=None):
     ``E / (k n^2) * sum_e counts[e] * sum_t p[t, e]`` over the n rows routed.
 
     Returns a Routing; ``gates`` and ``loss`` are differentiable if ``logits``
-    requires a gradient."""
+    requires a gradient, once: a second derivative raises WbError."""
     if stream is not None:
         return _on(stream, lambda: route(logits, k, mask, renormalize), logits, mask)
     if getattr(logits, "requires_grad", False) and _grad_enabled():
@@ -150,6 +150,17 @@ def _differentiable():
     if _apply is None:
         import torch
 
+        class Last(torch.autograd.Function):
+            """A gradient that depends on ``of``, which has no gradient itself: asking for one is an error."""
+
+            @staticmethod
+            def forward(ctx, d, *of):
+                return d.clone()
+
+            @staticmethod
+            def backward(ctx, *_):
+                raise WbError(WB_EUNSUPPORTED, "route's gradient has no gradient of its own")
+
         class Route(torch.autograd.Function):
             @staticmethod
             def forward(ctx, logits, k, mask, renormalize):
@@ -165,11 +176,13 @@ def _differentiable():
                 raise WbError(WB_EINVAL, "logits has a forward-mode tangent, which the operators do not carry on")
 
             @staticmethod
-            @torch.autograd.function.once_differentiable
             def backward(ctx, _e, d_gates, _p, _t, _c, _o, d_loss, _r):
                 logits, mask, experts, gates, counts, routed = ctx.saved_tensors
-                d = _backward(logits.detach(), experts, gates.detach(), counts, routed, mask,
-                              ctx.renormalize, d_gates.contiguous(), d_loss.contiguous())
+                with torch.no_grad():
+                    d = _backward(logits.detach(), experts, gates.detach(), counts, routed, mask,
+                                  ctx.renormalize, d_gates.contiguous(), d_loss.contiguous())
+                if torch.is_grad_enabled():  # create_graph
+                    d = Last.apply(d, logits, d_gates, d_loss)
                 return d, None, None, None
 
         _apply = Route.apply

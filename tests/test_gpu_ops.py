@@ -836,3 +836,18 @@ def test_norm_sum_and_routing_of_rows_far_apart():
     a, b = wb.route(far(x, apart), 6), wb.route(gpu(x), 6)
     assert all(torch.equal(u, v) for u, v in zip(a[:8], b[:8]))
     assert torch.equal(wb.route_backward(far(x, apart), a, torch.ones_like(a.gates)), wb.route_backward(gpu(x), b, torch.ones_like(b.gates)))
+
+
+def test_route_has_no_second_derivative_and_says_so():
+    z = torch.randn(6, 8, generator=torch.Generator().manual_seed(1)).cuda().requires_grad_()
+    first, = torch.autograd.grad(wb.route(z, 2).loss, z)
+    r = wb.route(z, 2)
+    d, = torch.autograd.grad(r.loss, z, create_graph=True)
+    assert torch.equal(d, first) and d.requires_grad
+    with pytest.raises(wb.WbError, match="no gradient of its own"):
+        (z.sum() + d.square().sum()).backward()
+    r = wb.route(z, 2)
+    weight = torch.ones(6, 2, device="cuda", requires_grad=True)
+    d, = torch.autograd.grad((r.gates * weight).sum(), z, create_graph=True)
+    with pytest.raises(wb.WbError, match="no gradient of its own"):
+        d.square().sum().backward()
