@@ -552,7 +552,7 @@ int wb_diff2_carry(const wb_field* fields, int32_t n, int32_t pass, int32_t last
  * wb_unpack leaves them, and the sum of a token's expert rows.
  *
  * Conventions, beside those above:
- *   - Each call enqueues one or two kernels on `stream` and returns; nothing is
+ *   - Each call enqueues one to three kernels on `stream` and returns; nothing is
  *     kept from one call for the next. Calls on different streams may overlap
  *     when their outputs and workspaces do not.
  *   - A wb_matrix is rows x cols elements, a row `ld` elements (>= cols) after

@@ -43,6 +43,8 @@ __device__ __forceinline__ float silu(float z) {
 // not below 2^-120), a third of the instructions (8192 rows, 28672 x 4096 bf16, gated:
 // 20 us of 1480).
 __device__ __forceinline__ float silu_to_bf16(float z) { return z * __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
+// 1 + erf loses relative precision far below zero, where the result is small:
+// it is off by roundings of z, as the same formula in elementary operations is.
 __device__ __forceinline__ float gelu(float z) { return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f)); }
 
 __device__ __forceinline__ void activate(float (&v)[4], int kind, int out_type) {
@@ -259,10 +261,11 @@ __device__ __forceinline__ int swizzle(int row) { return (row >> 1) & 7; }
 // What bounds it, as measured (rates of a large copy and of a large bf16
 // product on this card: 6.7 TB/s, 1.54 PFLOP/s):
 //   8192 rows, 28672 x 4096 bf16, gated    1.50 ms, 1.28 PFLOP/s: the matrix
-//     cores, 63 % of the cycles (the rest: barriers, operands from LDS)
+//     cores, 62 % of the cycles (the rest: barriers, operands from LDS)
 //   4096 rows, 7168 x 2048 fp8, and 8192 of 32 experts' 4096 x 7168, gated:
-//     0.14 and 0.67 ms, 0.88 and 0.72 PFLOP/s: widening and scaling in the
-//     vector units, beside matrix cores busy 35 to 41 %
+//     0.135 and 0.67 ms, 0.89 and 0.72 PFLOP/s: widening (in every wavefront that
+//     reads a code, so two or three times) and scaling in the vector units,
+//     beside matrix cores busy 38 to 40 %
 //   128 rows of the same 32 experts: 0.18 ms, the weight's bytes at 5.3 TB/s
 //   1 row, 6144 x 4096 bf16: 10 us, 5.0 TB/s with the launch and the call
 //   333 rows, 3442 x 1500 bf16, by way of registers: 18 us; 14 were the rows
@@ -750,7 +753,9 @@ hipError_t launch_tile(const LinearArgs& a, hipStream_t st) {
 }
 
 // The tiles in use. A launch takes the one whose rounds over the 256 CUs are
-// expected to be done first. A round takes us per stage of k (128 bytes of a
+// expected to be done first; memory's rate has no part in that (128 rows of 32
+// experts' 4096 x 7168 fp8: 75 us expected, 178 taken), nor do offsets, which
+// are on the device: every row of the result counts as some expert's. A round takes us per stage of k (128 bytes of a
 // row) and `fixed` for its start and its results; `resident` workgroups share
 // a CU. Measured with 1024 tiles, and with 256 (`few`: up to there every tile
 // has a CU to itself), for bf16 and fp8; the last two are us, with 512 and
@@ -775,7 +780,7 @@ constexpr Choice kChoices[] = {
     {128, 128, 1, {0.655f, 0.90f}, 5.0f, {0.74f, 0.914f}, 6.0f, {}, {}},
     {256, 256, 1, {1.5f, 3.24f}, 14.5f, {1.65f, 3.31f}, 11.5f, {}, {}},
 };
-constexpr double kCodesUs = 6.0;  // the second launch, and its workspace
+constexpr double kCodesUs = 6.0;  // the second launch, of few rows (8192 rows of 2048: 16 us, which is not priced)
 constexpr int kNumChoices = sizeof(kChoices) / sizeof(kChoices[0]);
 
 // Whether a tile holds whole scales of an fp8 output.

@@ -3,7 +3,7 @@ that unpacking leaves on a rollout rank (norm, router, products with plain and
 stacked weights, the sum of a token's expert rows), and the router's gradient
 for the trainer.
 
-Each function makes its outputs with torch, enqueues one or two HIP kernels of
+Each function makes its outputs with torch, enqueues one to three HIP kernels of
 libwb on the stream (the current one by default) and returns. Tensors are
 float32, bfloat16 or float8_e4m3fn in the memory of the current device; rows
 may lie any distance apart. fp8 activations go with float32 scales of one row
@@ -211,7 +211,8 @@ def expert_linear(x, weight, offsets, tokens=None, bias=None, *, x_scales=None, 
     ceil(K / 128)], bias [E, N]): row p of the result is of the expert with
     ``offsets[e] <= p < offsets[e + 1]`` (int32 [E + 1]; a rank's slice of
     Routing.offsets) and comes from row ``tokens[p]`` of x (int32), or from
-    row p without ``tokens``. Rows of no expert are left as they are."""
+    row p without ``tokens``. Rows of no expert hold nothing in particular:
+    the result is new memory that they are not written to."""
     if stream is not None:
         return _on(stream, lambda: expert_linear(x, weight, offsets, tokens, bias, x_scales=x_scales,
                                                  weight_scales=weight_scales, activation=activation, gated=gated,
