@@ -26,7 +26,7 @@ typedef uint32_t u32_a1 __attribute__((aligned(1)));
 
 constexpr int kStageBytes = 128;  // of a row, per step over k: a scale block of fp8, half as many bf16
 
-// Sixteen zero bytes: what a tile's 16-byte pieces past the end of k are read from.
+// Sixteen zero bytes: what a tile's 16-byte pieces and scales past the end of k are read from.
 __device__ const u32x4 zero_piece = {0, 0, 0, 0};
 
 // z / (1 + e^-z) by way of t = e^-|z|, which neither overflows nor takes its
@@ -336,10 +336,12 @@ __global__ __launch_bounds__(S::kThreads, 2) void wb_linear_tile_kernel(LinearAr
     }
   }
 
-  // the scale of a step that thread and round have to bring
-  auto scale_at = [&](int t, int i) {
-    const int h = min(tid + i * S::kThreads, S::STEP * S::kRows - 1) / S::kRows;
-    return scale_src[i] + min(t * S::STEP + h, stages - 1);
+  // the scale of a step that thread and round have to bring; zero of a stage past
+  // the end, whose sums are zeros (an infinite scale would make them NaN)
+  auto scale_at = [&](int t, int i) -> const float* {
+    if constexpr (S::STEP == 1) return scale_src[i] + t;
+    const int stage = t * S::STEP + min(tid + i * S::kThreads, S::STEP * S::kRows - 1) / S::kRows;
+    return stage < stages ? scale_src[i] + stage : reinterpret_cast<const float*>(&zero_piece);
   };
   auto send_scales = [&](int t, int slot) {
     if constexpr (F8) {

@@ -851,3 +851,20 @@ def test_route_has_no_second_derivative_and_says_so():
     d, = torch.autograd.grad((r.gates * weight).sum(), z, create_graph=True)
     with pytest.raises(wb.WbError, match="no gradient of its own"):
         d.square().sum().backward()
+
+
+@pytest.mark.parametrize("rows", [1, 40, 100])
+def test_an_infinite_scale_of_the_last_block_gives_infinities(rows):
+    """An odd number of blocks of 128, which tiles take two or four at a time: nothing is added for those past the end."""
+    f8, inf = torch.float8_e4m3fn, math.inf
+    for k in (128, 384, 640, 141, 400):
+        nb = ref.blocks(k)
+        x, w = torch.ones(rows, k).to(f8).cuda(), torch.ones(64, k).to(f8).cuda()
+        xs, ws = torch.ones(rows, nb, device="cuda"), torch.ones(1, nb, device="cuda")
+        xs[rows - 1, nb - 1] = inf
+        got = wb.linear(x, w, x_scales=xs, weight_scales=ws, out_dtype="f32")
+        assert torch.all(got[rows - 1] == inf) and torch.all(got[:rows - 1] == k), k
+        ws[0, nb - 1] = 1e30  # 1e30 twice is infinite as well
+        xs[rows - 1, nb - 1] = 1e30
+        got = wb.linear(x, w, x_scales=xs, weight_scales=ws, out_dtype="f32")
+        assert torch.all(got[rows - 1] == inf) and torch.isfinite(got[:rows - 1]).all(), k
