@@ -6,6 +6,7 @@
 // negative status.
 #include <ATen/ATen.h>
 #include <c10/core/GradMode.h>
+#include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdint>
@@ -124,16 +125,17 @@ PyObject* wrap(const Tensor& t) {
   return THPVariable_Wrap(t);
 }
 
+// A refusal becomes its text; what torch throws (no memory for a result) the
+// Python exception that torch has for it.
 template <class F>
 PyObject* guarded(F&& f) {
+  HANDLE_TH_ERRORS
   try {
     return f();
   } catch (const Refused& e) {
     return PyUnicode_FromString(e.what());
-  } catch (const std::exception& e) {
-    PyErr_SetString(PyExc_RuntimeError, e.what());
-    return nullptr;
   }
+  END_HANDLE_TH_ERRORS
 }
 
 bool counted(Py_ssize_t got, Py_ssize_t want, const char* call) {

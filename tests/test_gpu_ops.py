@@ -868,3 +868,11 @@ def test_an_infinite_scale_of_the_last_block_gives_infinities(rows):
         xs[rows - 1, nb - 1] = 1e30
         got = wb.linear(x, w, x_scales=xs, weight_scales=ws, out_dtype="f32")
         assert torch.all(got[rows - 1] == inf) and torch.isfinite(got[:rows - 1]).all(), k
+
+
+def test_a_result_that_memory_does_not_hold_is_torch_s_own_error():
+    """70 TB: programs that make room and try again wait for this type."""
+    x, w = torch.zeros(1 << 21, 8, dtype=torch.bfloat16, device="cuda"), torch.zeros(1 << 24, 8, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(torch.OutOfMemoryError):
+        wb.linear(x, w)
+    assert torch.all(wb.linear(x[:16], w[:16]) == 0)
