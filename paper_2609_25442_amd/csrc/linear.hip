@@ -732,7 +732,7 @@ int64_t col_tiles(const LinearArgs& a, int bn) {
   return (a.n_out + step - 1) / step;
 }
 
-constexpr int64_t kMaxTiles = 0x3fffff;  // of a launch: up to 512 threads each, 2^32 in all
+constexpr int64_t kMaxTiles = 0x3fffff;  // of a launch, whose threads (up to 512 a tile) stay below 2^32
 
 template <class S, bool F8, bool DIRECT>
 hipError_t launch_tile(const LinearArgs& a, hipStream_t st) {
@@ -757,15 +757,16 @@ hipError_t launch_tile(const LinearArgs& a, hipStream_t st) {
 // The tiles in use. A launch takes the one whose rounds over the 256 CUs are
 // expected to be done first; memory's rate has no part in that (128 rows of 32
 // experts' 4096 x 7168 fp8: 75 us expected, 178 taken), nor do offsets, which
-// are on the device: every row of the result counts as some expert's. A round takes us per stage of k (128 bytes of a
-// row) and `fixed` for its start and its results; `resident` workgroups share
-// a CU. Measured with 1024 tiles, and with 256 (`few`: up to there every tile
-// has a CU to itself), for bf16 and fp8; the last two are us, with 512 and
-// with 256 tiles, of rows that come by way of registers (0: not in use). Large
-// tiles read less per product; small ones give every CU work, and keep more of
-// the weight on its way when few rows meet it. 8192 x 8192 x 8192 bf16: 0.85
-// ms with 256 x 256, 0.99 with 128 x 128; 1024 x 7168 x 2048 fp8: 67 us and 37;
-// one row by 6144 x 4096 bf16: 12 us with 16 x 32, 31 with 64 x 64.
+// are on the device: every row of the result counts as some expert's. A round
+// takes us per stage of k (128 bytes of a row) and `fixed` for its start and
+// its results; `resident` workgroups share a CU. Measured with 1024 tiles, and
+// with 256 (`few`: up to there every tile has a CU to itself), for bf16 and
+// fp8; the last two are us, with 512 and with 256 tiles, of rows that come by
+// way of registers (0: not in use). Large tiles read less per product; small
+// ones give every CU work, and keep more of the weight on its way when few rows
+// meet it. 8192 x 8192 x 8192 bf16: 0.85 ms with 256 x 256, 0.99 with 128 x
+// 128; 1024 x 7168 x 2048 fp8: 67 us and 37; one row by 6144 x 4096 bf16: 12 us
+// with 16 x 32, 31 with 64 x 64.
 struct Choice {
   int bm, bn, resident;
   float us[2], fixed, few_us[2], few_fixed;
