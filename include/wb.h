@@ -669,6 +669,98 @@ int wb_linear(const wb_linear_args* args, void* workspace, size_t workspace_byte
 int wb_combine(const wb_matrix* y, const int32_t* positions, const float* gates, int32_t k, const wb_matrix* residual,
                const int32_t* first, const int32_t* last, const wb_matrix* out, void* stream);
 
+/* ---- operators around an MoE layer at the trainer -------------------------- */
+
+/* The lookup of token embeddings, the layer norm of a residual sum, rows sorted
+ * by expert and back, and the activation with a checkpoint in 8 bits, each with
+ * its gradient. The conventions of the operators above hold. Gradients are sums in
+ * fp32 in a fixed order, rounded once to their matrix's type; the types of a
+ * gradient and of what it is of may differ. */
+
+/* Token ids in device memory, one after the other: int32 (bytes 4) or int64 (8). At most 4194303. */
+typedef struct wb_tokens {
+  const void* data;
+  int32_t bytes;
+  int32_t reserved;
+  int64_t count;
+} wb_tokens;
+
+/* out[t] = scale * weight[tokens[t] - first]; a row of zeros where that is no
+ * row of the weight [V, cols] (a rank's part of a vocabulary: first >= 0 is the id
+ * of its first row). weight and out [count, cols] are WB_F32 or WB_BF16. V is at
+ * most 4194303. Errors: WB_EINVAL, WB_EUNSUPPORTED, WB_EHIP. */
+int wb_embedding(const wb_tokens* tokens, const wb_matrix* weight, float scale, int64_t first, const wb_matrix* out,
+                 void* stream);
+/* d_weight[v] = scale * sum of d_out[t] over tokens[t] - first == v, in the order
+ * of t; every row of d_weight is written. `workspace`: the bytes that
+ * wb_embedding_backward_workspace gives for as many tokens and columns and rows of
+ * d_weight, 16-byte aligned, free again when the call's work is done. Errors as
+ * wb_embedding, and WB_ESIZE. */
+int wb_embedding_backward_workspace(int64_t count, int64_t rows, int64_t cols, size_t* bytes);
+int wb_embedding_backward(const wb_tokens* tokens, const wb_matrix* d_out, float scale, int64_t first,
+                          const wb_matrix* d_weight, void* workspace, size_t workspace_bytes, void* stream);
+
+/* total = x + residual, rounded to total's type; over each row of it
+ *   out = (total - mean) * inv * weight + bias,  inv = 1 / sqrt(var + eps)
+ * with the row's mean and variance where `mean` is given, else with mean 0 and the
+ * mean square in place of the variance (no centring). Unlike wb_add_rms_norm, the
+ * norm sees the sum as it is kept: its gradient reads it again. residual and total
+ * go together (NULL both: total is x); bias may be NULL. mean (NULL: not centred)
+ * and inv are WB_F32 [rows], written for the gradient. Matrices are WB_F32 or
+ * WB_BF16, weight and bias [1, cols]. total may be x or residual itself, where the
+ * types are alike. eps >= 0. Errors: WB_EINVAL, WB_EUNSUPPORTED, WB_EHIP. */
+int wb_add_layer_norm(const wb_matrix* x, const wb_matrix* residual, const wb_matrix* weight, const wb_matrix* bias,
+                      float eps, const wb_matrix* total, const wb_matrix* out, float* mean, float* inv, void* stream);
+/* Gradients, with h = (total - mean) inv and g = d_out weight:
+ *   d_sum    = inv (g - mean of g - h * mean of g h) + d_total   (no mean of g without `mean`)
+ *   d_weight = sum over rows of d_out h,  d_bias = sum over rows of d_out
+ * total (x where there was no residual), mean and inv are the forward's. d_total
+ * (the gradient that total gets elsewhere) may be NULL. d_sum is written to d_x and,
+ * if given, to d_residual (its own type). d_weight and d_bias, [1, cols] of WB_F32 or
+ * WB_BF16, may be NULL; d_bias needs d_weight. d_x may be d_out or d_total itself, where
+ * the types are alike. `workspace`: wb_add_layer_norm_backward_workspace bytes,
+ * 16-byte aligned, free again when the call's work is done. Errors as
+ * wb_add_layer_norm, and WB_ESIZE. */
+int wb_add_layer_norm_backward_workspace(int64_t rows, int64_t cols, size_t* bytes);
+int wb_add_layer_norm_backward(const wb_matrix* d_out, const wb_matrix* total, const wb_matrix* weight,
+                               const wb_matrix* d_total, const float* mean, const float* inv, const wb_matrix* d_x,
+                               const wb_matrix* d_residual, const wb_matrix* d_weight, const wb_matrix* d_bias,
+                               void* workspace, size_t workspace_bytes, void* stream);
+
+/* Rows by expert: out[positions[t, i]] = x[t] for T rows of k choices, zeros in
+ * the other rows of out [places, cols] (those past the last place). positions [T, k] and
+ * tokens [places] are wb_routing's: positions[t, i] is a place of which tokens says t,
+ * and no place is named twice; what is not so, is outside 0..places-1, or
+ * outside first[0] <= place < last[0] where these device pointers are given, is
+ * left out. 1 <= k <= 64, places < 2^31. x and out are WB_F32 or WB_BF16.
+ * Errors: WB_EINVAL, WB_EUNSUPPORTED, WB_EHIP. */
+int wb_dispatch(const wb_matrix* x, const int32_t* positions, const int32_t* tokens, int32_t k, const int32_t* first,
+                const int32_t* last, const wb_matrix* out, void* stream);
+/* d_x[t] = sum over i of d_out[positions[t, i]], in the order of i; the same places are left out. */
+int wb_dispatch_backward(const wb_matrix* d_out, const int32_t* positions, const int32_t* tokens, int32_t k,
+                         const int32_t* first, const int32_t* last, const wb_matrix* d_x, void* stream);
+/* Gradients of wb_combine over wb_routing's places:
+ *   d_y[positions[t, i]] = gates[t, i] * d_out[t], zeros in y's other rows
+ *   d_gates[t, i] = sum over columns of d_out[t] * y[positions[t, i]], 0 where the place is left out
+ * (the residual's is d_out). Places as in wb_dispatch. y and d_gates may both be NULL, or
+ * d_y; y has d_y's shape. Errors as wb_dispatch. */
+int wb_combine_backward(const wb_matrix* d_out, const wb_matrix* y, const int32_t* positions, const int32_t* tokens,
+                        const float* gates, int32_t k, const int32_t* first, const int32_t* last, const wb_matrix* d_y,
+                        float* d_gates, void* stream);
+
+/* out = act(x), or with `gated`, where x's columns are [gate; up], act(gate) * up.
+ * x [T, N], out [T, N or N/2]: WB_F32 or WB_BF16. `codes` (WB_F8E4M3, x's shape) and
+ * `scales` (WB_F32, [T, ceil(N / 128)], gated [T, 2 ceil(N / 256)]) may both be NULL; else they get x
+ * in 8 bits, with a scale per 128 columns of a row, of each of its halves if gated,
+ * as the fp8 results above have them. Errors: WB_EINVAL, WB_EUNSUPPORTED, WB_EHIP. */
+int wb_activate(const wb_matrix* x, int32_t activation, int32_t gated, const wb_matrix* out, const wb_matrix* codes,
+                const wb_matrix* scales, void* stream);
+/* d_x from d_out and x; or, with scales given, from x's codes of wb_activate: the
+ * gradient at the values that they stand for. d_x has x's shape. It may be x
+ * itself, where the types are alike. */
+int wb_activate_backward(const wb_matrix* d_out, const wb_matrix* x, const wb_matrix* scales, int32_t activation,
+                         int32_t gated, const wb_matrix* d_x, void* stream);
+
 /* Message of the calling thread's last failed call ("" if none). */
 const char* wb_last_error(void);
 const char* wb_version(void);

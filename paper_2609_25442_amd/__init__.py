@@ -941,3 +941,6 @@ def allocate_locals(layout: Layout, rank: int, device="cuda", zero=False):
 
 from .ops import (Routing, add_rms_norm, combine, expert_linear, linear, route,  # noqa: E402,F401
                   route_backward)
+from .train import (Activated, NormGradient, Normed, activate, activate_backward, add_layer_norm,  # noqa: E402,F401
+                    add_layer_norm_backward, collect, collect_backward, dispatch, dispatch_backward, embedding,
+                    embedding_backward)

@@ -20,9 +20,10 @@ ARGS = os.path.join(HERE, "_args.so")
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 HIPCC = os.path.join(ROCM, "bin", "hipcc")
 
-HOST_SOURCES = ["api.cpp", "ops_api.cpp", "layout.cpp", "plan.cpp", "probe.cpp"]
-DEVICE_SOURCES = ["kernels.hip", "probe.hip", "noalloc.hip", "norm.hip", "route.hip", "linear.hip"]
-ARGS_SOURCES = ["args.cpp", "args_ops.cpp"]
+HOST_SOURCES = ["api.cpp", "ops_api.cpp", "train_api.cpp", "layout.cpp", "plan.cpp", "probe.cpp"]
+DEVICE_SOURCES = ["kernels.hip", "probe.hip", "noalloc.hip", "norm.hip", "route.hip", "linear.hip",
+                  "embedding.hip", "layer_norm.hip", "expert_rows.hip", "activate.hip"]
+ARGS_SOURCES = ["args.cpp", "args_ops.cpp", "args_train.cpp"]
 # no packed fp32 instructions: hipcc would otherwise form v_pk_*_f32 by itself;
 # a pointer that promises more alignment than its data has is an error, and so is
 # what nothing uses

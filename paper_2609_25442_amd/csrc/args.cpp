@@ -3,7 +3,7 @@
 // local tensors, and the checks run on every call). It answers only for plain
 // torch tensors that pass every check; for anything else it says no and the
 // binding's own Python checks decide, with their messages. The operators'
-// methods are in args_ops.cpp.
+// methods are in args_ops.cpp and args_train.cpp.
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdint>
@@ -88,6 +88,16 @@ PyMethodDef methods[] = {
     {"route_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(wb_py_route_backward)), METH_FASTCALL, nullptr},
     {"linear", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(wb_py_linear)), METH_FASTCALL, nullptr},
     {"combine", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(wb_py_combine)), METH_FASTCALL, nullptr},
+    {"embedding", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(wb_py_embedding)), METH_FASTCALL, nullptr},
+    {"embedding_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(wb_py_embedding_backward)), METH_FASTCALL, nullptr},
+    {"add_layer_norm", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(wb_py_add_layer_norm)), METH_FASTCALL, nullptr},
+    {"add_layer_norm_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(wb_py_add_layer_norm_backward)), METH_FASTCALL, nullptr},
+    {"dispatch", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(wb_py_dispatch)), METH_FASTCALL, nullptr},
+    {"dispatch_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(wb_py_dispatch_backward)), METH_FASTCALL, nullptr},
+    {"collect_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(wb_py_collect_backward)), METH_FASTCALL, nullptr},
+    {"activate", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(wb_py_activate)), METH_FASTCALL, nullptr},
+    {"activate_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(wb_py_activate_backward)), METH_FASTCALL, nullptr},
+    {"held_elsewhere", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(wb_py_held_elsewhere)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_args", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

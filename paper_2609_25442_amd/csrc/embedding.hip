@@ -1,0 +1,471 @@
+// Lookup of token embeddings, and the gradient of the table by sorted tokens.
+//   out_t = scale W[tok_t - first];   dW_v = scale sum_{t: tok_t - first = v} dout_t
+//
+// The lookup reads and writes a row per token. The gradient sorts the tokens
+// (stable, so that a row's sum goes by ascending t and does not depend on which
+// workgroup ran first), sums runs of equal tokens, and writes every row of dW
+// once, the ones without a token as zeros.
+#include <algorithm>
+
+#include "ops_device.hpp"
+#include "train.hpp"
+
+namespace wb {
+namespace {
+
+constexpr int kThreads = 256;
+
+// The row of a table of `rows` that token t names, or `rows` for none.
+__device__ __forceinline__ uint32_t row_of(const void* tokens, int bytes, int64_t t, int64_t first, int64_t rows) {
+  const int64_t id = bytes == 8 ? static_cast<const int64_t*>(tokens)[t] : int64_t(static_cast<const int32_t*>(tokens)[t]);
+  const uint64_t at = static_cast<uint64_t>(id) - static_cast<uint64_t>(first);  // first <= 2^62: nothing wraps into the rows
+  return static_cast<uint32_t>(at < static_cast<uint64_t>(rows) ? at : rows);
+}
+
+// ---- lookup ------------------------------------------------------------------
+
+template <int V, bool NT>
+__global__ __launch_bounds__(kThreads) void wb_embed_kernel(EmbedArgs a, int shift) {
+  const int lanes = 1 << shift, lane = threadIdx.x & (lanes - 1);
+  const int64_t row = int64_t(blockIdx.x) * (kThreads >> shift) + (threadIdx.x >> shift);
+  if (row >= a.count) return;
+  const uint32_t at = row_of(a.tokens, a.token_bytes, row, a.first, a.rows);
+  const char* w = static_cast<const char*>(a.weight) + int64_t(at) * a.ld_weight * bytes_of(a.weight_type);
+  char* out = static_cast<char*>(a.out) + row * a.ld_out * bytes_of(a.out_type);
+  const bool there = at < a.rows;
+  float v[V][8];
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const int64_t c = ((int64_t(blockIdx.y) * V + i) * lanes + lane) * 8;
+    if (c >= a.cols) break;
+    if (!there)
+      for (int j = 0; j < 8; ++j) v[i][j] = 0.0f;
+    else
+      load_run(w, c, a.cols, a.weight_type, v[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const int64_t c = ((int64_t(blockIdx.y) * V + i) * lanes + lane) * 8;
+    if (c >= a.cols) break;
+    if (there)
+      for (int j = 0; j < 8; ++j) v[i][j] *= a.scale;
+    store_run<NT>(out, c, a.cols, a.out_type, v[i]);
+  }
+}
+
+// ---- sort --------------------------------------------------------------------
+// Least significant digits first, stable. Up to kOneBlock tokens one workgroup
+// does every pass in LDS; above, a pass is two launches over blocks of tokens:
+// the digits' counts, then places.
+
+constexpr int kOneBlock = 8192, kOneThreads = 1024;
+constexpr int kSortThreads = 256, kSortItems = 8, kSortTile = kSortThreads * kSortItems, kMaxSortBlocks = 256;
+constexpr int kMaxDigits = 512;
+
+struct Passes {
+  int count, bits;  // of digits of `bits`
+};
+
+Passes passes_of(int64_t rows) {  // keys 0..rows
+  int bits = 1;
+  while ((rows >> bits) != 0) ++bits;
+  const int count = (bits + 8) / 9;
+  return {count, (bits + count - 1) / count};
+}
+
+int64_t sort_block(int64_t count) {
+  const int64_t per = (count + kMaxSortBlocks - 1) / kMaxSortBlocks;
+  return (per + kSortTile - 1) / kSortTile * kSortTile;
+}
+
+// The lanes below this one, and all, that hold the same digit.
+__device__ __forceinline__ uint64_t same_digit(uint32_t digit, int bits, bool on) {
+  uint64_t m = __ballot(on);
+  for (int b = 0; b < bits; ++b) {
+    const uint64_t with = __ballot((digit >> b) & 1);
+    m &= ((digit >> b) & 1) ? with : ~with;
+  }
+  return m;
+}
+
+__device__ __forceinline__ int lanes_below(uint64_t m) {
+  return __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(m >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(m), 0));
+}
+
+// Exclusive sums over `n` digits of LDS counts, one or more to a thread; `wave` holds one entry per wavefront.
+template <int THREADS>
+__device__ __forceinline__ void exclusive(uint32_t* counts, int n, uint32_t* wave) {
+  const int per = (n + THREADS - 1) / THREADS, tid = threadIdx.x;
+  uint32_t sum = 0;
+  for (int i = 0; i < per; ++i) sum += tid * per + i < n ? counts[tid * per + i] : 0;
+  uint32_t upto = sum;
+  for (int off = 1; off < 64; off <<= 1) {
+    const uint32_t o = __shfl_up(upto, off);
+    if ((tid & 63) >= off) upto += o;
+  }
+  if ((tid & 63) == 63) wave[tid >> 6] = upto;
+  __syncthreads();
+  uint32_t base = upto - sum;
+  for (int w = 0; w < (tid >> 6); ++w) base += wave[w];
+  for (int i = 0; i < per; ++i)
+    if (tid * per + i < n) {
+      const uint32_t c = counts[tid * per + i];
+      counts[tid * per + i] = base;
+      base += c;
+    }
+  __syncthreads();
+}
+
+// Up to kOneBlock tokens.
+__global__ __launch_bounds__(kOneThreads) void wb_sort_few_kernel(EmbedGradArgs a, uint32_t* keys, int32_t* order, int passes,
+                                                                  int bits) {
+  constexpr int kWaves = kOneThreads / 64, kItems = kOneBlock / kOneThreads;
+  __shared__ uint32_t key_at[kOneBlock];
+  __shared__ uint16_t from_at[kOneBlock];
+  __shared__ uint16_t seen[kWaves][kMaxDigits];  // per wavefront, of one digit; then where its next goes
+  __shared__ uint32_t counts[kMaxDigits], wave_sums[kWaves];
+  const int n = static_cast<int>(a.count), tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, digits = 1 << bits;
+  // a wavefront has consecutive tokens, 64 at a time
+  const int items = (n + kOneThreads - 1) / kOneThreads;
+  uint32_t key[kItems], rank[kItems];
+  uint32_t from[kItems];
+#pragma unroll
+  for (int i = 0; i < kItems; ++i) {
+    if (i >= items) break;
+    const int t = (wave * items + i) * 64 + lane;
+    from[i] = t;
+    key[i] = t < n ? row_of(a.tokens, a.token_bytes, t, a.first, a.rows) : 0xffffffffu;
+  }
+  for (int p = 0; p < passes; ++p) {
+    for (int d = tid; d < kWaves * digits; d += kOneThreads) seen[d >> bits][d & (digits - 1)] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+      if (i >= items) break;
+      const bool on = (wave * items + i) * 64 + lane < n;
+      const uint32_t digit = (key[i] >> (p * bits)) & (digits - 1);
+      const uint64_t same = same_digit(digit, bits, on);
+      const uint32_t before = seen[wave][digit];
+      rank[i] = before + lanes_below(same);
+      order_lanes();
+      if (on && lanes_below(same) == 0) seen[wave][digit] = static_cast<uint16_t>(before + __popcll(same));
+      order_lanes();
+    }
+    __syncthreads();
+    for (int d = tid; d < digits; d += kOneThreads) {
+      uint32_t sum = 0;
+      for (int w = 0; w < kWaves; ++w) {
+        const uint32_t c = seen[w][d];
+        seen[w][d] = static_cast<uint16_t>(sum);
+        sum += c;
+      }
+      counts[d] = sum;
+    }
+    __syncthreads();
+    exclusive<kOneThreads>(counts, digits, wave_sums);
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+      if (i >= items || (wave * items + i) * 64 + lane >= n) continue;
+      const uint32_t digit = (key[i] >> (p * bits)) & (digits - 1);
+      const uint32_t to = counts[digit] + seen[wave][digit] + rank[i];
+      key_at[to] = key[i];
+      from_at[to] = static_cast<uint16_t>(from[i]);
+    }
+    __syncthreads();
+    if (p + 1 < passes) {
+#pragma unroll
+      for (int i = 0; i < kItems; ++i) {
+        if (i >= items) break;
+        const int t = (wave * items + i) * 64 + lane;
+        if (t < n) key[i] = key_at[t], from[i] = from_at[t];
+      }
+    }
+  }
+  for (int t = tid; t < n; t += kOneThreads) {
+    keys[t] = key_at[t];
+    order[t] = from_at[t];
+  }
+}
+
+// Counts of a pass's digits by block, table[digit][block]. FIRST: the keys are
+// made from the tokens.
+template <bool FIRST>
+__global__ __launch_bounds__(kSortThreads) void wb_sort_count_kernel(EmbedGradArgs a, const uint32_t* keys, uint32_t* table,
+                                                                     int64_t per, int shift, int bits) {
+  __shared__ uint32_t counts[kMaxDigits];
+  const int digits = 1 << bits;
+  for (int d = threadIdx.x; d < digits; d += kSortThreads) counts[d] = 0;
+  __syncthreads();
+  const int64_t begin = int64_t(blockIdx.x) * per, end = min(begin + per, a.count);
+  for (int64_t t = begin + threadIdx.x; t < end; t += kSortThreads) {
+    const uint32_t key = FIRST ? row_of(a.tokens, a.token_bytes, t, a.first, a.rows) : keys[t];
+    atomicAdd(&counts[(key >> shift) & (digits - 1)], 1u);
+  }
+  __syncthreads();
+  for (int d = threadIdx.x; d < digits; d += kSortThreads) table[int64_t(d) * gridDim.x + blockIdx.x] = counts[d];
+}
+
+template <bool FIRST>
+__global__ __launch_bounds__(kSortThreads) void wb_sort_place_kernel(EmbedGradArgs a, const uint32_t* keys,
+                                                                     const int32_t* order, const uint32_t* table,
+                                                                     uint32_t* keys_to, int32_t* order_to, int64_t per,
+                                                                     int shift, int bits) {
+  constexpr int kWaves = kSortThreads / 64;
+  __shared__ uint32_t next[kMaxDigits], mine[kMaxDigits], wave_sums[kWaves];
+  __shared__ uint16_t seen[kWaves][kMaxDigits];
+  const int digits = 1 << bits, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, blocks = gridDim.x;
+  // a digit's first place: those of the smaller digits, and of this one in the blocks before
+  for (int d = tid; d < digits; d += kSortThreads) {
+    uint32_t all = 0, before = 0;
+    for (int b = 0; b < blocks; ++b) {
+      const uint32_t c = table[int64_t(d) * blocks + b];
+      all += c;
+      before += b < int(blockIdx.x) ? c : 0;
+    }
+    next[d] = all;
+    mine[d] = before;
+  }
+  __syncthreads();
+  exclusive<kSortThreads>(next, digits, wave_sums);
+  for (int d = tid; d < digits; d += kSortThreads) next[d] += mine[d];
+  __syncthreads();
+  const int64_t begin = int64_t(blockIdx.x) * per, end = min(begin + per, a.count);
+  for (int64_t tile = begin; tile < end; tile += kSortTile) {
+    for (int d = tid; d < kWaves * digits; d += kSortThreads) seen[d >> bits][d & (digits - 1)] = 0;
+    __syncthreads();
+    uint32_t key[kSortItems], rank[kSortItems];
+    int32_t from[kSortItems];
+#pragma unroll
+    for (int i = 0; i < kSortItems; ++i) {
+      const int64_t t = tile + (wave * kSortItems + i) * 64 + lane;
+      if (t >= end) continue;
+      key[i] = FIRST ? row_of(a.tokens, a.token_bytes, t, a.first, a.rows) : keys[t];
+      from[i] = FIRST ? static_cast<int32_t>(t) : order[t];
+    }
+#pragma unroll
+    for (int i = 0; i < kSortItems; ++i) {
+      const bool on = tile + (wave * kSortItems + i) * 64 + lane < end;
+      const uint32_t digit = on ? (key[i] >> shift) & (digits - 1) : 0;
+      const uint64_t same = same_digit(digit, bits, on);
+      const uint32_t before = seen[wave][digit];
+      rank[i] = before + lanes_below(same);
+      order_lanes();
+      if (on && lanes_below(same) == 0) seen[wave][digit] = static_cast<uint16_t>(before + __popcll(same));
+      order_lanes();
+    }
+    __syncthreads();
+    for (int d = tid; d < digits; d += kSortThreads) {
+      uint32_t sum = 0;
+      for (int w = 0; w < kWaves; ++w) {
+        const uint32_t c = seen[w][d];
+        seen[w][d] = static_cast<uint16_t>(sum);
+        sum += c;
+      }
+      mine[d] = sum;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kSortItems; ++i) {
+      if (tile + (wave * kSortItems + i) * 64 + lane >= end) continue;
+      const uint32_t digit = (key[i] >> shift) & (digits - 1);
+      const uint32_t to = next[digit] + seen[wave][digit] + rank[i];
+      keys_to[to] = key[i];
+      order_to[to] = from[i];
+    }
+    __syncthreads();
+    for (int d = tid; d < digits; d += kSortThreads) next[d] += mine[d];
+    __syncthreads();
+  }
+}
+
+// ---- sums --------------------------------------------------------------------
+// Sorted tokens are taken in chunks of kChunk. A run of equal tokens inside one
+// chunk is summed and written; one that goes over an end leaves an fp32 row
+// per chunk (0: the run that came in, 1: the one that goes on), which the second launch adds.
+
+constexpr int kChunk = 32;
+constexpr int kFillRows = 32;
+
+struct Sorted {
+  const uint32_t* keys;
+  const int32_t* order;
+  float* partial;  // [chunks][2][cols]
+  int64_t chunks;
+};
+
+__device__ __forceinline__ void store_scaled(const EmbedGradArgs& a, uint32_t v, int64_t c, float (&sum)[8]) {
+  char* to = static_cast<char*>(a.d_weight) + int64_t(v) * a.ld_d_weight * bytes_of(a.d_weight_type);
+  for (int j = 0; j < 8; ++j) sum[j] *= a.scale;
+  store_run(to, c, a.cols, a.d_weight_type, sum);
+}
+
+__global__ __launch_bounds__(kThreads) void wb_embed_sum_kernel(EmbedGradArgs a, Sorted s, int shift, int64_t chunk_blocks) {
+  const int lanes = 1 << shift, lane = threadIdx.x & (lanes - 1), sub = threadIdx.x >> shift, per = kThreads >> shift;
+  if (int64_t(blockIdx.x) >= chunk_blocks) {  // rows without a token
+    __shared__ uint32_t start[kFillRows + 1];
+    const int64_t v0 = (int64_t(blockIdx.x) - chunk_blocks) * kFillRows;
+    if (threadIdx.x <= kFillRows) {  // the first place of a key not below v0 + threadIdx.x
+      int64_t lo = 0, hi = a.count;
+      while (lo < hi) {
+        const int64_t mid = (lo + hi) >> 1;
+        if (s.keys[mid] < v0 + threadIdx.x)
+          lo = mid + 1;
+        else
+          hi = mid;
+      }
+      start[threadIdx.x] = static_cast<uint32_t>(lo);
+    }
+    __syncthreads();
+    const float none[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    for (int r = sub; r < kFillRows; r += per) {
+      const int64_t v = v0 + r;
+      if (v >= a.rows || start[r] != start[r + 1]) continue;
+      char* to = static_cast<char*>(a.d_weight) + v * a.ld_d_weight * bytes_of(a.d_weight_type);
+      for (int64_t c = (int64_t(blockIdx.y) * lanes + lane) * 8; c < a.cols; c += int64_t(gridDim.y) * lanes * 8) {
+        store_run(to, c, a.cols, a.d_weight_type, none);
+      }
+    }
+    return;
+  }
+  const int64_t chunk = int64_t(blockIdx.x) * per + sub;
+  const int64_t c = (int64_t(blockIdx.y) * lanes + lane) * 8;
+  if (chunk >= s.chunks || c >= a.cols) return;
+  const int64_t begin = chunk * kChunk, end = min(begin + kChunk, a.count);
+  const int db = a.d_out_type == WB_F32 ? 4 : 2;
+  float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  bool came = begin > 0 && s.keys[begin - 1] == s.keys[begin];  // the run began before this chunk
+  for (int64_t p = begin; p < end; ++p) {
+    const uint32_t v = s.keys[p];
+    if (v >= a.rows) break;  // tokens of other rows, sorted last
+    const char* row = static_cast<const char*>(a.d_out) + int64_t(s.order[p]) * a.ld_d_out * db;
+    float x[8];
+    load_run(row, c, a.cols, a.d_out_type, x);
+    for (int j = 0; j < 8; ++j) sum[j] += x[j];
+    const bool on = p + 1 < a.count && s.keys[p + 1] == v;
+    if (on && p + 1 < end) continue;
+    if (came || on) {
+      store_run(reinterpret_cast<char*>(s.partial + (chunk * 2 + (came ? 0 : 1)) * a.cols), c, a.cols, WB_F32, sum);
+    } else {
+      store_scaled(a, v, c, sum);
+    }
+    for (int j = 0; j < 8; ++j) sum[j] = 0.0f;
+    came = false;
+  }
+}
+
+// The runs that go over the end of the chunk they began in.
+__global__ __launch_bounds__(kThreads) void wb_embed_join_kernel(EmbedGradArgs a, Sorted s, int shift) {
+  const int lanes = 1 << shift, lane = threadIdx.x & (lanes - 1);
+  const int64_t chunk = int64_t(blockIdx.x) * (kThreads >> shift) + (threadIdx.x >> shift);
+  const int64_t c = (int64_t(blockIdx.y) * lanes + lane) * 8;
+  if (chunk + 1 >= s.chunks || c >= a.cols) return;
+  const int64_t begin = chunk * kChunk, end = begin + kChunk;
+  const uint32_t v = s.keys[end - 1];
+  if (v >= a.rows || s.keys[end] != v) return;
+  if (s.keys[begin] == v && begin > 0 && s.keys[begin - 1] == v) return;  // it began before
+  float sum[8], x[8];
+  auto load = [&](int64_t slot, float(&to)[8]) {
+    load_run(reinterpret_cast<const char*>(s.partial + slot * a.cols), c, a.cols, WB_F32, to);
+  };
+  load(chunk * 2 + 1, sum);
+  for (int64_t next = chunk + 1; next < s.chunks && s.keys[next * kChunk] == v; ++next) {
+    load(next * 2, x);
+    for (int j = 0; j < 8; ++j) sum[j] += x[j];
+  }
+  store_scaled(a, v, c, sum);
+}
+
+int64_t up16(int64_t n) { return (n + 15) / 16 * 16; }
+
+// What of the workspace lies where, in bytes.
+struct Layout {
+  int64_t keys[2], order[2], table, partial, all;
+};
+
+Layout layout_of(int64_t count, int64_t rows, int64_t cols) {
+  Layout l{};
+  int64_t at = 0;
+  const auto take = [&](int64_t bytes) {
+    const int64_t here = at;
+    at += up16(bytes);
+    return here;
+  };
+  const bool few = count <= kOneBlock;
+  for (int i = 0; i < (few ? 1 : 2); ++i) l.keys[i] = take(count * 4), l.order[i] = take(count * 4);
+  if (!few) l.table = take((int64_t(4) << passes_of(rows).bits) * kMaxSortBlocks);
+  l.partial = take(count > kChunk ? (count + kChunk - 1) / kChunk * 2 * cols * 4 : 0);
+  l.all = at;
+  return l;
+}
+
+}  // namespace
+
+size_t embed_grad_workspace_bytes(int64_t count, int64_t rows, int64_t cols) {
+  return static_cast<size_t>(layout_of(count, rows, cols).all);
+}
+
+int launch_embed(const EmbedArgs& a, void* stream) {
+  if (a.count == 0) return hipSuccess;
+  const auto st = static_cast<hipStream_t>(stream);
+  const int shift = row_shift(a.cols);
+  const int64_t per = kThreads >> shift, runs = (a.cols + 7) / 8;
+  const int64_t lanes = int64_t(1) << shift;
+  const auto go = [&](auto kernel, int v) {
+    hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>((a.count + per - 1) / per), static_cast<uint32_t>((runs + lanes * v - 1) / (lanes * v))),
+                       dim3(kThreads), 0, st, a, shift);
+    return hipGetLastError();
+  };
+  const bool nt = a.count * a.cols * (bytes_of(a.weight_type) + bytes_of(a.out_type)) > kStreamBytes;
+  if (runs <= lanes) return nt ? go(wb_embed_kernel<1, true>, 1) : go(wb_embed_kernel<1, false>, 1);
+  return nt ? go(wb_embed_kernel<2, true>, 2) : go(wb_embed_kernel<2, false>, 2);
+}
+
+int launch_embed_grad(const EmbedGradArgs& a, void* stream) {
+  const auto st = static_cast<hipStream_t>(stream);
+  char* ws = static_cast<char*>(a.workspace);
+  const Layout l = layout_of(a.count, a.rows, a.cols);
+  const Passes p = passes_of(a.rows);
+  const auto keys = [&](int i) { return reinterpret_cast<uint32_t*>(ws + l.keys[i]); };
+  const auto order = [&](int i) { return reinterpret_cast<int32_t*>(ws + l.order[i]); };
+  int now = 0;
+  if (a.count > 0 && a.count <= kOneBlock) {
+    hipLaunchKernelGGL(wb_sort_few_kernel, dim3(1), dim3(kOneThreads), 0, st, a, keys(0), order(0), p.count, p.bits);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  } else if (a.count > 0) {
+    const int64_t per = sort_block(a.count);
+    const dim3 grid(static_cast<uint32_t>((a.count + per - 1) / per));
+    auto* table = reinterpret_cast<uint32_t*>(ws + l.table);
+    for (int i = 0; i < p.count; ++i) {
+      const int from = now, to = i == 0 ? 0 : 1 - now, shift = i * p.bits;
+      if (i == 0) {
+        hipLaunchKernelGGL(wb_sort_count_kernel<true>, grid, dim3(kSortThreads), 0, st, a, nullptr, table, per, shift, p.bits);
+        hipLaunchKernelGGL(wb_sort_place_kernel<true>, grid, dim3(kSortThreads), 0, st, a, nullptr, nullptr, table, keys(to),
+                           order(to), per, shift, p.bits);
+      } else {
+        hipLaunchKernelGGL(wb_sort_count_kernel<false>, grid, dim3(kSortThreads), 0, st, a, keys(from), table, per, shift, p.bits);
+        hipLaunchKernelGGL(wb_sort_place_kernel<false>, grid, dim3(kSortThreads), 0, st, a, keys(from), order(from), table,
+                           keys(to), order(to), per, shift, p.bits);
+      }
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+      now = to;
+    }
+  }
+  Sorted s{};
+  s.keys = keys(now), s.order = order(now), s.partial = reinterpret_cast<float*>(ws + l.partial);
+  s.chunks = (a.count + kChunk - 1) / kChunk;
+  const int shift = row_shift(a.cols);
+  const int64_t per = kThreads >> shift, slab = int64_t(8) << shift;
+  const int64_t blocks = (s.chunks + per - 1) / per, fills = (a.rows + kFillRows - 1) / kFillRows;
+  const uint32_t slabs = static_cast<uint32_t>((a.cols + slab - 1) / slab);
+  if (blocks + fills == 0) return hipSuccess;
+  hipLaunchKernelGGL(wb_embed_sum_kernel, dim3(static_cast<uint32_t>(blocks + fills), slabs), dim3(kThreads), 0, st, a, s, shift,
+                     blocks);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || s.chunks < 2) return e;
+  hipLaunchKernelGGL(wb_embed_join_kernel, dim3(static_cast<uint32_t>(blocks), slabs), dim3(kThreads), 0, st, a, s, shift);
+  return hipGetLastError();
+}
+
+}  // namespace wb

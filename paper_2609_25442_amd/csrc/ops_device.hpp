@@ -129,6 +129,31 @@ __device__ __forceinline__ void store_tail(void* row, int64_t col, int64_t cols,
     if (col + i < cols) store_one(row, col + i, type, v[i]);
 }
 
+// Eight columns of a row that may end before the eighth.
+template <bool NT = false>
+__device__ __forceinline__ void load_run(const char* row, int64_t c, int64_t cols, int type, float (&v)[8]) {
+  if (c + 8 <= cols)
+    load_eight<NT>(row, c, type, v);
+  else
+    load_tail(row, c, cols, type, v);
+}
+
+template <bool NT = false>
+__device__ __forceinline__ void store_run(char* row, int64_t c, int64_t cols, int type, const float (&v)[8]) {
+  if (c + 8 <= cols)
+    store_eight<NT>(row, c, type, v);
+  else
+    store_tail(row, c, cols, type, v);
+}
+
+// Lanes of a workgroup of 256 over rows: 1 << row_shift lanes hold a row's runs
+// of eight columns, wider rows all of them.
+inline int row_shift(int64_t cols) {
+  int shift = 3;
+  while (shift < 8 && (int64_t(8) << shift) < cols) ++shift;
+  return shift;
+}
+
 // Four neighbouring columns.
 typedef u32x2 u32x2_a2 __attribute__((aligned(2)));
 

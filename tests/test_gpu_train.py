@@ -1,0 +1,740 @@
+"""The trainer's operators on the GPU against their formulas in 64 bits
+(train_ref), alone and as one layer, at the sizes, types, strides, masks and
+calls where they can go wrong."""
+
+import math
+
+import pytest
+import torch
+
+import ops_ref as ref
+import paper_2609_25442_amd as wb
+import train_ref as tr
+from gpu_util import say
+
+pytestmark = pytest.mark.gpu
+T = ref.TORCH
+
+
+def gpu(t):
+    return None if t is None else t.cuda()
+
+
+def same(a, b):
+    return (a is None and b is None) or (a.dtype == b.dtype and torch.equal(a, b))
+
+
+def draw_tokens(shape, vocab, seed, kind=torch.int64, extra=0.0):
+    """Ids of which a few are frequent, and some outside 0..vocab-1."""
+    g = torch.Generator().manual_seed(seed)
+    n = math.prod(shape)
+    ids = (torch.rand(n, generator=g, dtype=torch.float64) * math.log(vocab + 1)).exp().long() - 1
+    ids = torch.where(torch.rand(n, generator=g) < 0.2, vocab // 2, ids.clamp(0, vocab - 1))
+    wrong = torch.randint(-3, 2 * vocab + 3, (n,), generator=g)
+    return torch.where(torch.rand(n, generator=g) < extra, wrong, ids).to(kind).view(shape)
+
+
+# ---- embeddings --------------------------------------------------------------------------------
+
+EMBED = [(1, 1, 1), (1, 7, 8), (3, 5, 64), (0, 9, 16), (40, 3, 129), (100, 1000, 72), (33, 2, 2049), (65, 40, 4100),
+         (1000, 300, 513), (31, 513, 8), (32, 600, 40), (8192, 700, 24), (8193, 700, 24), (20000, 262200, 8), (70000, 37, 16)]
+
+
+@pytest.mark.parametrize("shape", EMBED, ids=lambda s: "x".join(map(str, s)))
+def test_embedding_and_its_gradient(shape):
+    count, vocab, cols = shape
+    say("embedding", shape)
+    for seed, (wt, out, dt, dwt, kind, scale, first) in enumerate([
+            ("bf16", None, "bf16", None, torch.int64, 1.0, 0), ("f32", "bf16", "f32", "bf16", torch.int32, 8.5, 0),
+            ("bf16", "f32", "bf16", "f32", torch.int64, -0.3, 2), ("f32", None, "f32", None, torch.int32, 1.0, vocab // 2)]):
+        tokens = draw_tokens((count,), vocab, seed, kind, 0.3 if first else 0.0)
+        scale32 = float(torch.tensor(scale))
+        w = ref.randn(vocab, cols, seed=seed, dtype=wt)
+        got = wb.embedding(gpu(tokens), gpu(w), scale=scale, first=first, out_dtype=out)
+        assert got.dtype == T[out or wt] and got.shape == (count, cols)
+        ref.check(got, *tr.embedding(tokens.long(), w, scale32, first), "lookup")
+        d = ref.randn(count, cols, seed=seed + 50, dtype=dt)
+        back = wb.embedding_backward(gpu(d), gpu(tokens), vocab, scale=scale, first=first, out_dtype=dwt)
+        assert back.dtype == T[dwt or dt] and back.shape == (vocab, cols)
+        ref.check(back, *tr.embedding_backward(d, tokens.long(), vocab, scale32, first), "gradient")
+
+
+def test_embedding_of_any_shape_of_tokens():
+    w = ref.randn(50, 24, seed=1)
+    for shape in ((), (2, 3), (4, 1, 5), (2, 0, 3)):
+        tokens = draw_tokens(shape, 50, 3)
+        got = wb.embedding(gpu(tokens), gpu(w))
+        assert got.shape == (*shape, 24) and torch.equal(got.cpu(), w[tokens])
+        d = ref.randn(*shape, 24, seed=2)
+        back = wb.embedding_backward(gpu(d), gpu(tokens), 50)
+        ref.check(back, *tr.embedding_backward(d, tokens, 50, 1.0, 0), shape)
+
+
+@pytest.mark.parametrize("ids", ["all the same", "all different", "all outside", "far outside", "runs of a chunk"])
+def test_embedding_gradient_of_special_tokens(ids):
+    n, vocab, cols = 9000, 9000, 40
+    say("embedding", ids)
+    tokens = {"all the same": torch.full((n,), 8999), "all different": torch.randperm(n, generator=torch.Generator().manual_seed(1)),
+              "all outside": torch.full((n,), vocab), "runs of a chunk": torch.arange(n) // 32,
+              "far outside": torch.tensor([-2 ** 63, 2 ** 63 - 1, -1, vocab] * (n // 4))}[ids]
+    d = ref.randn(n, cols, seed=2, dtype="f32")
+    for m in (n, 4097, 64, 33, 32, 31):
+        back = wb.embedding_backward(gpu(d[:m]), gpu(tokens[:m]), vocab)
+        ref.check(back, *tr.embedding_backward(d[:m], tokens[:m], vocab, 1.0, 0), m)
+
+
+@pytest.mark.parametrize("pad,skip", [(0, 1), (3, 0), (5, 3)])
+@pytest.mark.parametrize("cols", [5, 264, 1501])
+def test_embedding_of_rows_that_start_anywhere(cols, pad, skip):
+    say("embedding strided", cols, pad, skip)
+    tokens = draw_tokens((70,), 30, 4)
+    for t in ("bf16", "f32"):
+        w, d = ref.randn(30, cols, seed=1, dtype=t), ref.randn(70, cols, seed=2, dtype=t)
+        got = wb.embedding(gpu(tokens), ref.strided(w, pad, skip))
+        assert torch.equal(got.cpu(), w[tokens])
+        back = wb.embedding_backward(ref.strided(d, pad, skip), gpu(tokens), 30)
+        assert torch.equal(back, wb.embedding_backward(gpu(d), gpu(tokens), 30))
+
+
+def test_embedding_keeps_what_is_not_finite_to_its_rows():
+    w = ref.randn(6, 20, seed=1)
+    w[2, 3], w[4, 0] = math.nan, math.inf
+    tokens = torch.tensor([0, 2, 4, 9, 5])
+    got = wb.embedding(gpu(tokens), gpu(w), scale=2.0).cpu()
+    assert torch.isnan(got[1, 3]) and got[2, 0] == math.inf and torch.all(got[3] == 0)
+    assert torch.isfinite(got).sum() == got.numel() - 2
+    d = torch.zeros(5, 20)
+    d[1, 1], d[3] = math.inf, math.nan
+    back = wb.embedding_backward(gpu(d), gpu(tokens), 6).cpu()
+    assert back[2, 1] == math.inf and torch.isfinite(back).sum() == back.numel() - 1
+
+
+def test_embedding_parts_of_a_vocabulary_add_up():
+    tokens, w = draw_tokens((64,), 100, 5), ref.randn(100, 48, seed=1)
+    whole = wb.embedding(gpu(tokens), gpu(w))
+    parts = [wb.embedding(gpu(tokens), gpu(w[lo:hi]), first=lo) for lo, hi in ((0, 40), (40, 99), (99, 100))]
+    assert torch.equal(sum(parts), whole)
+
+
+def test_embedding_of_rows_past_four_gigabytes():
+    say("embedding, far rows")
+    vocab, cols = 300000, 8192
+    w = torch.zeros(vocab, cols, dtype=torch.bfloat16, device="cuda")
+    tokens = torch.tensor([vocab - 1, 0, 270000, vocab - 1], device="cuda")
+    w[vocab - 1], w[270000] = 3.0, 2.0
+    assert wb.embedding(tokens, w)[:, ::97].float().mean(1).tolist() == [3.0, 0.0, 2.0, 3.0]
+    del w
+    back = wb.embedding_backward(torch.ones(4, cols, dtype=torch.bfloat16, device="cuda"), tokens, vocab)
+    want = torch.zeros(vocab, device="cuda")
+    want[tokens[:3]] = torch.tensor([2.0, 1.0, 1.0], device="cuda")
+    assert torch.equal(back[:, 8191].float(), want) and torch.equal(back[:, 0].float(), want)
+
+
+# ---- layer norm --------------------------------------------------------------------------------
+
+NORM = [(1, 1), (1, 7), (3, 8), (5, 127), (4, 128), (2, 129), (3, 512), (70, 513), (5, 1000), (9, 1501), (3, 2050), (300, 96),
+        (4, 4096), (2100, 136), (33, 4100), (3, 7168), (5, 8200), (2, 16390), (1, 32768), (3, 40001), (0, 64)]
+
+
+@pytest.mark.parametrize("center", [True, False], ids=["centred", "rms"])
+@pytest.mark.parametrize("shape", NORM, ids=lambda s: "x".join(map(str, s)))
+def test_layer_norm_and_its_gradient(shape, center):
+    rows, cols = shape
+    say("layer norm", shape, center)
+    for seed, (xt, rt, wt, bt, out, dt) in enumerate([
+            ("bf16", "bf16", "bf16", "bf16", None, "bf16"), ("f32", None, "f32", "f32", None, "f32"),
+            ("bf16", "f32", "f32", None, "f32", "f32"), ("f32", "bf16", "bf16", "f32", "bf16", "bf16"),
+            ("bf16", None, "f32", None, None, "f32")]):
+        x = ref.randn(rows, cols, seed=seed, dtype=xt, scale=3.0) + (0.5 if xt == "f32" else 0)
+        r = ref.randn(rows, cols, seed=seed + 50, dtype=rt) if rt else None
+        w = ref.randn(cols, seed=seed + 100, dtype=wt, scale=0.2) + torch.ones((), dtype=T[wt])
+        b = ref.randn(cols, seed=seed + 150, dtype=bt) if bt else None
+        n = wb.add_layer_norm(gpu(x), gpu(w), gpu(b), gpu(r), eps=1e-3, center=center, out_dtype=out)
+        f = tr.layer_norm(x, w, b, r, float(torch.tensor(1e-3)), center)
+        assert n.out.dtype == T[out or xt] and torch.equal(n.total.cpu(), f["total"])
+        assert (n.mean is None) == (not center)
+        ref.check(n.inv, f["inv"][:, 0], f["e_inv"][:, 0], "inv")
+        if center:
+            ref.check(n.mean, f["mean"][:, 0], f["e_mean"][:, 0], "mean")
+        ref.check(n.out, f["out"], f["e_out"], "norm")
+        d = ref.randn(rows, cols, seed=seed + 200, dtype=dt)
+        more = ref.randn(rows, cols, seed=seed + 250, dtype=rt) if rt else None
+        got = wb.add_layer_norm_backward(gpu(d), n, gpu(w), d_total=gpu(more))
+        of_sum, of_w, of_b = tr.layer_norm_backward(f, w, d, more, center)
+        assert got.x.dtype == T[xt] and (got.residual is None) == (r is None) and (got.bias is None) == (b is None)
+        ref.check(got.x, *of_sum, "gradient of x")
+        if r is not None:
+            assert got.residual.dtype == T[rt]
+            ref.check(got.residual, *of_sum, "gradient of the residual")
+        assert got.weight.dtype == T[wt] and got.weight.shape == (cols,)
+        ref.check(got.weight, *of_w, "gradient of the weight")
+        if b is not None:
+            assert got.bias.dtype == T[bt]
+            ref.check(got.bias, *of_b, "gradient of the bias")
+
+
+@pytest.mark.parametrize("pad,skip", [(0, 1), (3, 0), (5, 3)])
+@pytest.mark.parametrize("cols", [5, 264, 1500, 4099, 8193])
+def test_layer_norm_of_rows_that_start_anywhere(cols, pad, skip):
+    say("layer norm strided", cols, pad, skip)
+    for t in ("bf16", "f32"):
+        x, r, d, m = (ref.randn(6, cols, seed=s, dtype=t) for s in range(4))
+        w = ref.randn(cols, seed=4, dtype=t)
+        n = wb.add_layer_norm(gpu(x), gpu(w), gpu(w), gpu(r))
+        far = wb.add_layer_norm(*(ref.strided(x, pad, skip), gpu(w), gpu(w), ref.strided(r, pad, skip)))
+        assert all(same(a, b) for a, b in zip(n[:4], far[:4]))
+        there = wb.add_layer_norm_backward(gpu(d), n, gpu(w), gpu(m))
+        back = wb.add_layer_norm_backward(ref.strided(d, pad, skip), n._replace(total=ref.strided(n.total.cpu(), pad, skip)),
+                                          gpu(w), ref.strided(m, pad, skip))
+        assert all(same(a, b) for a, b in zip(there, back))
+
+
+def test_layer_norm_gradient_against_differences():
+    """A rounding of eps to fp32 aside, the gradient is that of the formula's value."""
+    rows, cols = 4, 11
+    x, w, b, d = ref.randn(rows, cols, seed=1), ref.randn(cols, seed=2), ref.randn(cols, seed=3), ref.randn(rows, cols, seed=4)
+    for center in (True, False):
+        n = wb.add_layer_norm(gpu(x), gpu(w), gpu(b), eps=2.0 ** -10, center=center)
+        got = wb.add_layer_norm_backward(gpu(d), n, gpu(w))
+
+        def value(x, w, b):
+            t = x - (x.mean(1, keepdim=True) if center else 0)
+            return ((t * (t.pow(2).mean(1, keepdim=True) + 2.0 ** -10).rsqrt() * w + b) * d.double()).sum()
+
+        at, h = [x.double(), w.double(), b.double()], 1e-6
+        for which, g in enumerate((got.x, got.weight, got.bias)):
+            for i in range(g.numel()):
+                v = [t.clone() for t in at]
+                v[which].view(-1)[i] += h
+                up = value(*v)
+                v[which].view(-1)[i] -= 2 * h
+                # third derivatives here are below 1e4, the values below 1e3 with 2^-53 of them lost
+                assert abs(float(g.view(-1)[i]) - float(up - value(*v)) / (2 * h)) < 1e-5 + 1e-5 * abs(float(g.view(-1)[i]))
+
+
+def test_layer_norm_of_equal_and_not_finite_values():
+    x = torch.full((6, 300), 5.0)
+    x[1, 7], x[3, 0], x[4] = math.nan, math.inf, 0.0
+    w, b, d = torch.ones(300), torch.full((300,), 2.0), torch.ones(6, 300)
+    n = wb.add_layer_norm(gpu(x), gpu(w), gpu(b), eps=1e-5)
+    out = n.out.cpu()
+    assert torch.all(torch.isnan(out[[1, 3]])) and torch.all(out[[0, 2, 4, 5]] == 2.0)
+    assert torch.all(n.inv.cpu()[[0, 2, 4, 5]] > 300)
+    got = wb.add_layer_norm_backward(gpu(d), n, gpu(w)).x.cpu()
+    assert torch.all(torch.isnan(got[[1, 3]])) and torch.all(got[[0, 2, 4, 5]] == 0)
+    zero = wb.add_layer_norm(gpu(torch.zeros(2, 9)), gpu(w[:9]), eps=0.0, center=False)
+    assert torch.all(torch.isinf(zero.inv)) and torch.all(torch.isnan(zero.out))
+
+
+def test_layer_norm_without_centring_is_the_rms_norm():
+    x, w = ref.randn(50, 640, seed=1, dtype="bf16").cuda(), ref.randn(640, seed=2, dtype="bf16").cuda()
+    a, b = wb.add_layer_norm(x, w, eps=1e-6, center=False, out_dtype="f32").out, wb.add_rms_norm(x, w, out_dtype="f32")[0]
+    assert torch.all((a - b).abs() <= 8 * ref.U32 * b.abs())
+
+
+# ---- rows by expert and back -------------------------------------------------------------------
+
+
+def routing(rows, experts, k, seed, masked=0.0):
+    z = ref.randn(rows, experts, seed=seed)
+    mask = torch.rand(rows, generator=torch.Generator().manual_seed(seed)) >= masked if masked else None
+    r = wb.route(gpu(z), k, mask=gpu(mask))
+    return r, {f: getattr(r, f).cpu().long() for f in ("positions", "tokens", "offsets")}
+
+
+PLACES = [(1, 1, 1, 1), (3, 5, 2, 7), (5, 8, 8, 129), (16, 4, 2, 2048), (40, 64, 6, 2056), (7, 100, 64, 40), (9, 6, 3, 4099),
+          (300, 12, 3, 512), (33, 8, 2, 8200), (2, 4, 4, 20001), (1000, 256, 8, 64), (0, 8, 2, 16)]
+
+
+@pytest.mark.parametrize("masked", [0.0, 0.4, 1.1], ids=["all", "some", "none"])
+@pytest.mark.parametrize("shape", PLACES, ids=lambda s: "x".join(map(str, s)))
+def test_dispatch_and_collect_with_their_gradients(shape, masked):
+    rows, experts, k, cols = shape
+    say("dispatch", shape, masked)
+    r, want = routing(rows, experts, k, 3, masked)
+    mid = [int(want["offsets"][i]) for i in (experts // 3, (2 * experts + 2) // 3)]
+    for t, dt, span in (("bf16", "bf16", None), ("f32", "f32", None), ("bf16", "f32", mid), ("f32", "bf16", [0, 0])):
+        on = None if span is None else torch.tensor([span[0], 5, span[1]], dtype=torch.int32, device="cuda")
+        x, y, res = (ref.randn(n, cols, seed=s, dtype=t) for s, n in ((1, rows), (2, rows * k), (3, rows)))
+        assert torch.equal(wb.dispatch(gpu(x), r, span=on).cpu(), tr.dispatch(x, want, span)), span
+        d = ref.randn(rows * k, cols, seed=4, dtype=dt)
+        back = wb.dispatch_backward(gpu(d), r, span=on, out_dtype=t)
+        assert back.dtype == T[t]
+        ref.check(back, *tr.dispatch_backward(d, want, span), f"gradient of dispatch {span}")
+        for gates in (None, ref.randn(rows, k, seed=5)):
+            g = r.gates.cpu() if gates is None else gates
+            out = wb.collect(gpu(y), r, gates=gpu(gates), residual=gpu(res), span=on)
+            assert torch.equal(out, wb.combine(gpu(y), r.positions, gpu(g), residual=gpu(res), span=on))
+            d_out = ref.randn(rows, cols, seed=6, dtype=dt)
+            d_y, d_g = wb.collect_backward(gpu(d_out), gpu(y), r, gates=gpu(gates), span=on)
+            of_y, of_g = tr.collect_backward(d_out, y, want, g, span)
+            assert d_y.dtype == T[t] and d_g.dtype == torch.float32
+            ref.check(d_y, *of_y, f"gradient of y {span}")
+            ref.check(d_g, *of_g, f"gradient of the gates {span}")
+
+
+@pytest.mark.parametrize("pad,skip", [(0, 1), (3, 0), (5, 3)])
+@pytest.mark.parametrize("cols", [5, 264, 1501, 4099])
+def test_dispatch_and_collect_of_rows_that_start_anywhere(cols, pad, skip):
+    say("dispatch strided", cols, pad, skip)
+    r, _ = routing(20, 6, 3, 1, 0.2)
+    far = lambda t: ref.strided(t, pad, skip)  # noqa: E731
+    for t in ("bf16", "f32"):
+        x, y, d = ref.randn(20, cols, seed=1, dtype=t), ref.randn(60, cols, seed=2, dtype=t), ref.randn(20, cols, seed=3, dtype=t)
+        assert torch.equal(wb.dispatch(far(x), r), wb.dispatch(gpu(x), r))
+        assert torch.equal(wb.dispatch_backward(far(y), r), wb.dispatch_backward(gpu(y), r))
+        assert all(same(a, b) for a, b in zip(wb.collect_backward(far(d), far(y), r), wb.collect_backward(gpu(d), gpu(y), r)))
+
+
+def test_places_that_are_no_rows_own_are_left_out():
+    """Integers that no router wrote: outside the places, or of places that name another row, twice in other rows."""
+    i = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    r, _ = routing(3, 4, 2, 1)
+    r = r._replace(positions=i(0, 9, -7, 2, 2, 4).view(3, 2), tokens=i(0, 0, 1, 7, -9, 2147483647),
+                   gates=torch.tensor([[2.0, math.nan], [math.inf, 4.0], [math.nan, 5.0]], device="cuda"))
+    x, d, y = (ref.randn(n, 40, seed=n).cuda() for n in (3, 3, 6))
+    out, (d_y, d_g) = wb.dispatch(x, r), wb.collect_backward(d, y, r)
+    assert torch.equal(out[0], x[0]) and torch.equal(out[2], x[1]) and torch.all(out[[1, 3, 4, 5]] == 0)
+    assert torch.equal(d_y[0], 2 * d[0]) and torch.equal(d_y[2], 4 * d[1]) and torch.all(d_y[[1, 3, 4, 5]] == 0)
+    assert torch.all(d_g[[0, 1, 2, 2], [1, 0, 0, 1]] == 0) and torch.all(d_g[[0, 1], [0, 1]] != 0)
+    back = wb.dispatch_backward(y, r)
+    assert torch.equal(back[0], y[0]) and torch.equal(back[1], y[2]) and torch.all(back[2] == 0)
+
+
+def test_what_unused_places_hold_goes_nowhere():
+    r, want = routing(50, 8, 2, 1, 0.5)
+    places = int(want["offsets"][-1])
+    y = ref.randn(100, 72, seed=1)
+    clean = y.clone()
+    y[places:], clean[places:] = math.nan, 0
+    d = ref.randn(50, 72, seed=2).cuda()
+    assert torch.equal(wb.dispatch_backward(gpu(y), r), wb.dispatch_backward(gpu(clean), r))
+    assert all(torch.equal(a, b) for a, b in zip(wb.collect_backward(d, gpu(y), r), wb.collect_backward(d, gpu(clean), r)))
+    assert torch.equal(wb.collect(gpu(y), r), wb.collect(gpu(clean), r))
+
+
+def test_collect_computes_only_the_gradients_asked_for():
+    r, _ = routing(30, 8, 2, 1)
+    r = r._replace(gates=r.gates.detach())
+    y, d = ref.randn(60, 200, seed=1).cuda(), ref.randn(30, 200, seed=2).cuda()
+    d_y, d_g = wb.collect_backward(d, y, r)
+    for need_y, need_g in ((True, False), (False, True)):
+        a, g = y.clone().requires_grad_(need_y), r.gates.clone().requires_grad_(need_g)
+        wb.collect(a, r, gates=g).backward(d)
+        assert same(a.grad, d_y if need_y else None) and same(g.grad, d_g if need_g else None)
+
+
+def test_dispatch_past_four_gigabytes():
+    say("dispatch, far rows")
+    rows, cols, k = 70000, 8192, 4
+    r, want = routing(rows, 8, k, 1)
+    x = torch.zeros(rows, cols, dtype=torch.bfloat16, device="cuda")
+    x[:, 8191] = (torch.arange(rows, device="cuda") % 251).bfloat16()
+    out = wb.dispatch(x, r)
+    assert torch.equal(out[:, 8191], x[r.tokens.long(), 8191]) and not out[:, 0].any()
+    d_x = wb.dispatch_backward(out, r)
+    assert torch.equal(d_x[:, 8191], 4 * x[:, 8191])
+    d_y, d_g = wb.collect_backward(x, out, r)
+    assert torch.equal(d_g[:, 0], x[:, 8191].float() ** 2)
+    assert torch.equal(d_y[-1, 8191], (r.gates[r.tokens[-1].long()][r.positions[r.tokens[-1].long()] == rows * k - 1][0]
+                                       * x[r.tokens[-1].long(), 8191].float()).bfloat16())
+
+
+# ---- activation --------------------------------------------------------------------------------
+
+ACT = [(1, 1), (1, 8), (3, 127), (2, 128), (5, 129), (4, 300), (3, 1501), (2, 4100), (2, 14336), (700, 24), (0, 16)]
+
+
+@pytest.mark.parametrize("gated", [False, True], ids=["plain", "gated"])
+@pytest.mark.parametrize("kind", ["none", "silu", "gelu"])
+@pytest.mark.parametrize("shape", ACT, ids=lambda s: "x".join(map(str, s)))
+def test_activation_and_its_gradient(shape, kind, gated):
+    rows, cols = shape
+    say("activate", shape, kind, gated)
+    for seed, (xt, out, dt) in enumerate([("bf16", None, "bf16"), ("f32", None, "f32"), ("bf16", "f32", "f32"), ("f32", "bf16", "bf16")]):
+        x = ref.randn(rows, cols * (2 if gated else 1), seed=seed, dtype=xt, scale=3.0)
+        d = ref.randn(rows, cols, seed=seed + 50, dtype=dt)
+        for keep in (False, True):
+            a = wb.activate(gpu(x), kind, gated=gated, checkpoint=keep, out_dtype=out)
+            assert a.out.dtype == T[out or xt] and a.out.shape == (rows, cols)
+            ref.check(a.out, *tr.activate(x, kind, gated), "activation")
+            z, off = x.double(), 0.0
+            if keep:
+                codes, scales = tr.kept(x, gated)
+                assert torch.equal(a.saved.view(torch.uint8).cpu(), codes.view(torch.uint8)), "codes"
+                assert torch.equal(a.scales.cpu(), scales), "scales"
+                z, off = tr.kept_values(codes, scales, gated), ref.U32
+            got = wb.activate_backward(gpu(d), a)
+            assert got.dtype == T[xt] and got.shape == x.shape
+            ref.check(got, *tr.activate_backward(d, z, kind, gated, off), f"gradient, keep {keep}")
+
+
+@pytest.mark.parametrize("pad,skip", [(0, 1), (3, 0), (5, 3)])
+@pytest.mark.parametrize("cols", [5, 264, 1501])
+def test_activation_of_rows_that_start_anywhere(cols, pad, skip):
+    say("activate strided", cols, pad, skip)
+    for t in ("bf16", "f32"):
+        x, d = ref.randn(6, 2 * cols, seed=1, dtype=t), ref.randn(6, cols, seed=2, dtype=t)
+        for keep in (False, True):
+            a, b = (wb.activate(v, "silu", gated=True, checkpoint=keep) for v in (gpu(x), ref.strided(x, pad, skip)))
+            assert same(a.out, b.out) and same(a.scales, b.scales)
+            assert torch.equal(wb.activate_backward(gpu(d), a), wb.activate_backward(ref.strided(d, pad, skip), b))
+
+
+@pytest.mark.parametrize("kind", ["silu", "gelu"])
+def test_activation_gradient_against_differences(kind):
+    """Over both tails and the bend, in steps of 1/64."""
+    x = torch.arange(-800, 800, dtype=torch.float64)[None] / 64
+    got = wb.activate_backward(torch.ones(1, 1600, device="cuda"), wb.activate(x.float().cuda(), kind)).double().cpu()
+    h = 1e-5
+    diff = (tr.curve(x + h, kind)[0] - tr.curve(x - h, kind)[0]) / (2 * h)
+    # h^2 / 6 of third derivatives below 2, and 2^-52 of values below 13 over h; the slope's own bound
+    bound = h * h + 13 * 2.0 ** -52 / h + tr.curve(x, kind)[3]
+    assert torch.all((got - diff).abs() <= bound + ref.U32 * diff.abs())
+
+
+def test_activation_of_the_ends():
+    x = torch.tensor([[3e38, -3e38, 200.0, -200.0, 0.0, -0.0, 1e-40, math.nan]])
+    for kind in ("silu", "gelu"):
+        a = wb.activate(x.cuda(), kind)
+        assert a.out.cpu()[0, :6].tolist() == [x[0, 0], 0, 200, 0, 0, 0] and torch.isnan(a.out[0, 7])
+        d = wb.activate_backward(torch.ones(1, 8, device="cuda"), a).cpu()[0]
+        assert d[:6].tolist() == [1, 0, 1, 0, 0.5, 0.5] and torch.isnan(d[7])
+
+
+def test_checkpoints_of_not_finite_and_smallest_values():
+    x = ref.randn(4, 300, seed=1)
+    x[0, 3], x[1, 200] = math.nan, math.inf
+    x[2, :128], x[3, 128:256] = 0.0, 608 * 2.0 ** -149
+    a = wb.activate(x.cuda(), "silu", checkpoint=True)
+    codes, s = a.saved.float().cpu(), a.scales.cpu()
+    assert torch.isnan(codes[0, 3]) and torch.isfinite(codes[0]).sum() == 299 and torch.isnan(codes[1, 200])
+    assert s[2, 0] == 1 and torch.all(codes[2, :128] == 0) and s[1, 1] == math.inf
+    assert torch.all(codes[3, 128:256] == 448) and s[3, 1] == 2.0 ** -149
+    d = wb.activate_backward(torch.ones(4, 300, device="cuda"), a).cpu()
+    assert torch.isnan(d[0, 3]) and torch.isfinite(d[0]).sum() == 299 and torch.all(torch.isfinite(d[2:]))
+
+
+# ---- graphs, streams, captures -------------------------------------------------------------------
+
+
+def layer(tokens, p, residual, keep=True, span=None):
+    """A trainer's MoE layer on embedded tokens: norm, router, experts between dispatch and collect."""
+    x = wb.embedding(tokens, p["table"], scale=4.0)
+    n = wb.add_layer_norm(x, p["norm"], p["shift"], residual)
+    r = wb.route(n.out.float() @ p["router"].t(), 2)
+    rows = wb.dispatch(n.out, r)
+    at = r.offsets.tolist()
+    up = torch.cat([rows[at[e]:at[e + 1]] @ p["w13"][e].t() for e in range(len(at) - 1)] + [rows[at[-1]:] @ p["w13"][0].t()])
+    act = wb.activate(up, "silu", gated=True, checkpoint=keep).out
+    y = torch.cat([act[at[e]:at[e + 1]] @ p["w2"][e].t() for e in range(len(at) - 1)] + [act[at[-1]:] @ p["w2"][0].t()])
+    return wb.collect(y, r, residual=n.total), r, n
+
+
+def params(hidden, ffn, experts, vocab):
+    shapes = dict(table=(vocab, hidden), norm=(hidden,), shift=(hidden,), router=(experts, hidden), w13=(experts, 2 * ffn, hidden),
+                  w2=(experts, hidden, ffn))
+    return {n: ref.randn(*s, seed=i, scale=0.3).cuda().requires_grad_() for i, (n, s) in enumerate(shapes.items())}
+
+
+@pytest.mark.parametrize("count", [1, 50])
+def test_a_layer_of_them_all(count):
+    """Every gradient against torch's own in 64 bits, with the choices of experts fixed."""
+    say("layer", count)
+    hidden, ffn, experts, vocab = 72, 40, 5, 30
+    p = params(hidden, ffn, experts, vocab)
+    tokens, residual = draw_tokens((count,), vocab, 1).cuda(), ref.randn(count, hidden, seed=9).cuda().requires_grad_()
+    out, r, n = layer(tokens, p, residual, keep=False)
+    d = ref.randn(count, hidden, seed=10).cuda()
+    ((out * d).sum() + r.loss).backward()
+    q = {k: v.detach().double().cpu().requires_grad_() for k, v in p.items()}
+    res, ids = residual.detach().double().cpu().requires_grad_(), tokens.cpu()
+    total = q["table"][ids] * 4 + res
+    h = (total - total.mean(1, keepdim=True)) * (total.var(1, unbiased=False, keepdim=True) + 1e-5).rsqrt() * q["norm"] + q["shift"]
+    z = h @ q["router"].t()
+    chosen = r.experts.cpu().long()
+    gates = torch.softmax(z.gather(1, chosen), 1)
+    want = total
+    for i in range(2):
+        g, up = torch.bmm(q["w13"][chosen[:, i]], h[..., None])[..., 0].chunk(2, 1)
+        want = want + gates[:, i:i + 1] * torch.bmm(q["w2"][chosen[:, i]], (g * torch.sigmoid(g) * up)[..., None])[..., 0]
+    loss = experts / (2 * count ** 2) * (r.counts.cpu().double() * torch.softmax(z, 1).sum(0)).sum()
+    ((want * d.double().cpu()).sum() + loss).backward()
+    # fp32 throughout: every value and gradient is a sum of at most a few hundred products of numbers of order 1 to 100
+    close = lambda a, b: float((a.double().cpu() - b).abs().max()) <= 2e-4 * float(b.abs().max())  # noqa: E731
+    assert close(out.detach(), want.detach()) and close(residual.grad, res.grad)
+    for k in p:
+        assert close(p[k].grad, q[k].grad), k
+
+
+def test_a_layer_with_checkpoints_in_8_bits_gives_the_gradient_at_what_they_stand_for():
+    x, d = ref.randn(9, 400, seed=1).cuda().requires_grad_(), ref.randn(9, 200, seed=2).cuda()
+    a = wb.activate(x, "gelu", gated=True, checkpoint=True)
+    assert a.saved.dtype == torch.float8_e4m3fn and not a.saved.requires_grad and not a.scales.requires_grad
+    a.out.backward(d)
+    kept = tr.kept_values(a.saved.cpu(), a.scales.cpu(), True)
+    ref.check(x.grad, *tr.activate_backward(d.cpu(), kept, "gelu", True, ref.U32), "gradient")
+    assert torch.equal(x.grad, wb.activate_backward(d, a))
+
+
+def autograd_calls():
+    """name -> (function of its leaves, leaves, the same gradients without a graph)"""
+    r, _ = routing(20, 6, 2, 1, 0.2)
+    r = r._replace(gates=r.gates.detach())
+    f = lambda n, c, s, t="bf16": ref.randn(n, c, seed=s, dtype=t).cuda()  # noqa: E731
+    tokens = draw_tokens((20,), 15, 1).cuda()
+    w, x, res, y = f(15, 48, 1), f(20, 48, 2), f(20, 48, 3, "f32"), f(40, 48, 4)
+    nw, nb = f(1, 48, 5)[0].contiguous(), f(1, 48, 6, "f32")[0].contiguous()
+
+    def norm(d):
+        g = wb.add_layer_norm_backward(d, wb.add_layer_norm(x, nw, nb, res), nw)
+        return g.x, g.weight, g.bias, g.residual
+
+    return {
+        "embedding": (lambda w: wb.embedding(tokens, w, scale=3.0), [w], lambda d: (wb.embedding_backward(d, tokens, 15, scale=3.0),)),
+        "add_layer_norm": (lambda x, w, b, r: wb.add_layer_norm(x, w, b, r).out, [x, nw, nb, res], norm),
+        "dispatch": (lambda x: wb.dispatch(x, r), [x], lambda d: (wb.dispatch_backward(d, r),)),
+        "collect": (lambda y, g, s: wb.collect(y, r, gates=g, residual=s), [y, r.gates, x],
+                    lambda d: (*wb.collect_backward(d, y, r), d)),
+        "activate": (lambda x: wb.activate(x, "silu", gated=True).out, [x],
+                     lambda d: (wb.activate_backward(d, wb.activate(x, "silu", gated=True)),)),
+    }
+
+
+NAMES = ["embedding", "add_layer_norm", "dispatch", "collect", "activate"]
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_graphs_give_the_same_gradients_as_the_calls_without(name):
+    call, leaves, plain = autograd_calls()[name]
+    leaves = [t.detach().clone().requires_grad_() for t in leaves]
+    out = call(*leaves)
+    d = ref.randn(*out.shape, seed=3).to(out.dtype).cuda()
+    out.backward(d, retain_graph=True)
+    for t, want in zip(leaves, plain(d)):
+        assert t.grad.dtype == t.dtype and torch.equal(t.grad, want)
+    # once more into the same gradients; expanded and transposed gradients; half of the leaves
+    first = [t.grad.clone() for t in leaves]
+    out.backward(d, retain_graph=True)
+    assert all(torch.equal(t.grad, 2 * a) for t, a in zip(leaves, first))
+    ones = torch.autograd.grad(out.sum(), leaves, retain_graph=True)
+    assert all(torch.equal(a, b) for a, b in zip(ones, plain(torch.ones_like(out))))
+    turned = torch.autograd.grad(out, leaves, d.t().contiguous().t(), retain_graph=True)
+    assert all(torch.equal(a, b) for a, b in zip(turned, first))
+    for i, t in enumerate(leaves):
+        part = [u.detach().requires_grad_(u is t) for u in leaves]
+        call(*part).backward(d)
+        assert torch.equal(part[i].grad, first[i]) and sum(u.grad is not None for u in part) == 1
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_second_derivatives_and_tangents_raise(name):
+    import torch.autograd.forward_ad as fw
+
+    call, leaves, plain = autograd_calls()[name]
+    leaves = [t.detach().clone().requires_grad_() for t in leaves]
+    out = call(*leaves)
+    d = torch.ones_like(out).requires_grad_()
+    first = torch.autograd.grad(out, leaves, d, create_graph=True)
+    ours = [g for t, g in zip(leaves, first) if not (name == "collect" and t is leaves[2])]  # the residual's is torch's own
+    for g in ours:
+        with pytest.raises(wb.WbError, match="no gradient of its own"):
+            torch.autograd.grad(g.float().sum(), d, retain_graph=True)
+    with pytest.raises(wb.WbError, match="requires a gradient"):
+        plain(d)
+    for i in range(len(leaves)):
+        for keeps in (False, True):
+            with fw.dual_level():
+                dual = [t.detach().clone().requires_grad_(keeps) for t in leaves]
+                dual[i] = fw.make_dual(dual[i], torch.ones_like(dual[i]))
+                with pytest.raises(wb.WbError, match="tangent"):
+                    call(*dual)
+
+
+def test_only_the_sum_of_a_norm_may_go_on():
+    x, w, r = (t.requires_grad_() for t in (torch.ones(3, 8, device="cuda").bfloat16(), torch.ones(8, device="cuda"),
+                                            torch.ones(3, 8, device="cuda")))
+    n = wb.add_layer_norm(x, w, None, r)
+    n.total.sum().backward()
+    assert torch.all(x.grad == 1) and x.grad.dtype == torch.bfloat16 and torch.all(r.grad == 1) and w.grad is None
+    y = torch.ones(3, 8, device="cuda", requires_grad=True)
+    assert wb.add_layer_norm(y, w).total is y
+
+
+def test_a_changed_input_is_noticed_before_its_gradient():
+    x = ref.randn(4, 16, seed=1).cuda().requires_grad_()
+    y = x * 1
+    out = wb.activate(y, "silu").out
+    with torch.no_grad():
+        y.zero_()
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        out.sum().backward()
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_on_a_stream_of_its_own(name):
+    call, leaves, plain = autograd_calls()[name]
+    want = call(*leaves)
+    d = ref.randn(*want.shape, seed=3).to(want.dtype).cuda()
+    grads = plain(d)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        own = [t.detach().clone().requires_grad_() for t in leaves]
+        out = call(*own)
+        out.backward(d)
+    s.synchronize()
+    assert torch.equal(out, want) and all(torch.equal(t.grad, g) for t, g in zip(own, grads))
+
+
+def test_stream_arguments():
+    r, _ = routing(20, 6, 2, 1)
+    tokens = draw_tokens((20,), 15, 1).cuda()
+    x, w, y = ref.randn(20, 48, seed=1).cuda(), ref.randn(15, 48, seed=2).cuda(), ref.randn(40, 48, seed=3).cuda()
+    n, a = wb.add_layer_norm(x, w[0]), wb.activate(x, "gelu", checkpoint=True)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    calls = [lambda **k: wb.embedding(tokens, w, **k), lambda **k: wb.embedding_backward(x, tokens, 15, **k),
+             lambda **k: wb.add_layer_norm(x, w[0], **k), lambda **k: wb.add_layer_norm_backward(x, n, w[0], **k),
+             lambda **k: wb.dispatch(x, r, **k), lambda **k: wb.dispatch_backward(y, r, **k), lambda **k: wb.collect(y, r, **k),
+             lambda **k: wb.collect_backward(x, y, r, **k), lambda **k: wb.activate(x, "gelu", checkpoint=True, **k),
+             lambda **k: wb.activate_backward(x, a, **k)]
+    flat = lambda v: [t for t in (v if isinstance(v, tuple) else (v,)) if isinstance(t, torch.Tensor)]  # noqa: E731
+    for call in calls:
+        there, here = flat(call(stream=s)), flat(call(stream=s.cuda_stream))
+        s.synchronize()
+        bits = lambda t: t.view(torch.uint8) if t.dtype == torch.float8_e4m3fn else t  # noqa: E731
+        assert all(torch.equal(bits(u), bits(v)) and torch.equal(bits(u), bits(t)) for u, v, t in zip(there, here, flat(call())))
+
+
+def test_results_do_not_change_from_call_to_call():
+    tokens = draw_tokens((30000,), 50, 1).cuda()
+    d, x, w = ref.randn(30000, 64, seed=1).cuda(), ref.randn(3000, 1024, seed=2).cuda(), ref.randn(1024, seed=3).cuda()
+    n = wb.add_layer_norm(x, w)
+    first = wb.embedding_backward(d, tokens, 50), wb.add_layer_norm_backward(x, n, w).weight
+    for _ in range(5):
+        again = wb.embedding_backward(d, tokens, 50), wb.add_layer_norm_backward(x, n, w).weight
+        assert all(torch.equal(a, b) for a, b in zip(first, again))
+
+
+def step_inputs(count, seed):
+    return [draw_tokens((count,), 40, seed).cuda()] + [ref.randn(count, 96, seed=seed + s).cuda() for s in range(3)]
+
+
+def step(tokens, residual, d_out, d_total, p):
+    """A forward and backward pass through all of them, without a graph."""
+    x = wb.embedding(tokens, p["table"], scale=2.0)
+    n = wb.add_layer_norm(x, p["norm"], p["shift"], residual)
+    r = wb.route(n.out @ p["router"], 2)
+    rows = wb.dispatch(n.out, r)
+    a = wb.activate(rows, "silu", gated=True, checkpoint=True)
+    y = a.out @ p["down"]
+    out = wb.collect(y, r, residual=n.total)
+    d_y, d_gates = wb.collect_backward(d_out, y, r)
+    d_logits = wb.route_backward(n.out @ p["router"], r, d_gates, p["d_loss"])
+    d_h = wb.dispatch_backward(wb.activate_backward(d_y @ p["down"].t(), a), r) + d_logits @ p["router"].t()
+    g = wb.add_layer_norm_backward(d_h, n, p["norm"], d_total=d_out + d_total)
+    return [out, g.weight, g.bias, g.residual, wb.embedding_backward(g.x, tokens, 40, scale=2.0), d_gates]
+
+
+@pytest.mark.parametrize("count", [40, 9000])
+def test_a_step_in_a_graph(count):
+    """Captured twice on one pool, while a graph of the same leaves lives, and replayed in turns on new inputs with eager
+    work between."""
+    say("captured step", count)
+    shapes = dict(table=(40, 96), norm=(96,), shift=(96,), router=(96, 8), down=(48, 96))
+    p = {n: ref.randn(*s, seed=20 + i, scale=0.3).cuda().requires_grad_() for i, (n, s) in enumerate(shapes.items())}
+    p["d_loss"] = torch.ones((), device="cuda")
+    alive = wb.embedding(torch.zeros(3, dtype=torch.int64, device="cuda"), p["table"])
+    alive = wb.add_layer_norm(alive, p["norm"], p["shift"]).out
+    held = [step_inputs(count, s) for s in (100, 200)]
+    with torch.no_grad():
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            step(*held[0], p)
+        torch.cuda.current_stream().wait_stream(side)
+        graphs, outs = [torch.cuda.CUDAGraph() for _ in held], []
+        pool = torch.cuda.graph_pool_handle()
+        for g, inputs in zip(graphs, held):
+            with torch.cuda.graph(g, pool=pool):
+                outs.append(step(*inputs, p))
+        for i in range(6):
+            which = (i // 2 + i) % 2
+            for t, new in zip(held[which], step_inputs(count, 300 + i)):
+                t.copy_(new)
+            graphs[which].replay()
+            torch.cuda.synchronize()
+            want = step(*held[which], p)
+            assert all(torch.equal(a, b) for a, b in zip(outs[which], want)), i
+    alive.sum().backward()
+    assert p["table"].grad is not None
+
+
+def test_a_capture_over_leaves_of_a_living_graph_is_refused():
+    w = ref.randn(30, 64, seed=1).cuda().requires_grad_()
+    tokens = draw_tokens((9,), 30, 1).cuda()
+    alive = wb.embedding(tokens, w)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        with pytest.raises(wb.WbError, match="another stream"):
+            wb.embedding(tokens, w)
+        y = wb.embedding(tokens, w.detach())
+    g.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(y, alive)
+    # without one it is captured, gradient and all
+    del alive
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        wb.embedding(tokens, w).backward(torch.ones(9, 64, device="cuda"))
+    torch.cuda.current_stream().wait_stream(side)
+    want, w.grad = w.grad.clone(), None
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        wb.embedding(tokens, w).backward(torch.ones(9, 64, device="cuda"))
+    for _ in range(3):
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(w.grad, want)
+
+
+def test_refusals():
+    f = lambda *s, dt=torch.bfloat16: torch.zeros(*s, dtype=dt, device="cuda")  # noqa: E731
+    x, w, v, ids = f(4, 64), f(9, 64), f(64), torch.zeros(4, dtype=torch.int64, device="cuda")
+    r, _ = routing(4, 8, 2, 1)
+    y, f8, f32 = f(8, 64), torch.float8_e4m3fn, torch.float32
+    n, a, k = wb.add_layer_norm(x, v), wb.activate(x), wb.activate(x, checkpoint=True)
+    bad = [
+        lambda: wb.embedding(ids.cpu(), w), lambda: wb.embedding(ids, w.cpu()), lambda: wb.embedding(ids.float(), w),
+        lambda: wb.embedding(ids.short(), w), lambda: wb.embedding(ids.view(2, 2).t(), w), lambda: wb.embedding(ids, w[0]),
+        lambda: wb.embedding(ids, w.half()), lambda: wb.embedding(ids, w, first=-1), lambda: wb.embedding(ids, w.t()),
+        lambda: wb.embedding(ids, w, out_dtype="f8e4m3"), lambda: wb.embedding(ids, w, out_dtype="f16"), lambda: wb.embedding(None, w),
+        lambda: wb.embedding(ids, w, first=2 ** 63 - 1), lambda: wb.embedding(ids, f(9, 64, dt=f8)),
+        lambda: wb.embedding_backward(x[:3], ids, 9), lambda: wb.embedding_backward(x, ids, -1),
+        lambda: wb.embedding_backward(x, ids, 1 << 23), lambda: wb.embedding_backward(x.t(), ids, 9),
+        lambda: wb.add_layer_norm(x, v[:63]), lambda: wb.add_layer_norm(x, v, v[:63]), lambda: wb.add_layer_norm(x, v, eps=-1.0),
+        lambda: wb.add_layer_norm(x, v, eps=math.nan), lambda: wb.add_layer_norm(x, v, residual=f(4, 63)),
+        lambda: wb.add_layer_norm(x, v, residual=f(3, 64)), lambda: wb.add_layer_norm(x, v, out_dtype="f8e4m3"),
+        lambda: wb.add_layer_norm(x, None), lambda: wb.add_layer_norm(x[0], v), lambda: wb.add_layer_norm(x.t(), f(4)),
+        lambda: wb.add_layer_norm_backward(f(4, 63), n, v), lambda: wb.add_layer_norm_backward(x, n, f(63)),
+        lambda: wb.add_layer_norm_backward(x, n, v, d_total=f(3, 64)), lambda: wb.add_layer_norm_backward(x, n._replace(inv=v), v),
+        lambda: wb.add_layer_norm_backward(x, n._replace(x_type=torch.float16), v),
+        lambda: wb.dispatch(f(5, 64), r), lambda: wb.dispatch(x.half(), r), lambda: wb.dispatch(x, r, span=ids),
+        lambda: wb.dispatch(x, r._replace(tokens=r.tokens.long())), lambda: wb.dispatch(x, r._replace(positions=ids)),
+        lambda: wb.dispatch(f(4, 64, dt=f8), r), lambda: wb.dispatch_backward(f(7, 64), r),
+        lambda: wb.dispatch_backward(y, r, out_dtype="f8e4m3"), lambda: wb.collect(f(9, 64), r), lambda: wb.collect(y, r, gates=f(4, 2)),
+        lambda: wb.collect(y, r, residual=f(5, 64)), lambda: wb.collect_backward(f(5, 64), y, r), lambda: wb.collect_backward(x, f(8, 65), r),
+        lambda: wb.collect_backward(x, f(9, 64), r), lambda: wb.collect_backward(x, y, r, gates=f(4, 2)),
+        lambda: wb.activate(x, "tanh"), lambda: wb.activate(f(4, 63), gated=True), lambda: wb.activate(x, out_dtype="f8e4m3"),
+        lambda: wb.activate(x.to(f8)), lambda: wb.activate(v), lambda: wb.activate_backward(f(4, 63), a),
+        lambda: wb.activate_backward(x, a._replace(gated=True)), lambda: wb.activate_backward(x, k._replace(scales=None)),
+        lambda: wb.activate_backward(x, a._replace(scales=k.scales)), lambda: wb.activate_backward(x, k._replace(scales=f(4, 2, dt=f32))),
+    ]
+    for i, call in enumerate(bad):
+        with pytest.raises(wb.WbError) as e:
+            call()
+        assert str(e.value), i
+    torch.cuda.synchronize()
