@@ -3,8 +3,13 @@
 //   g = dout w;  dt = inv (g - mean(g) - h mean(g h)) + dtotal;  dw = sum_rows dout h,  db = sum_rows dout
 // or without centring: mean 0, and the mean square in place of the variance.
 //
-// Forward, a row is held in registers between its two sums (mean, then squares
-// of what is left) and its result, as in norm.hip.
+// Bandwidth bound. Forward, a row is held in registers between its two sums
+// (mean, then squares of what is left) and its result, as in norm.hip: 16384 x
+// 4096 bf16 with a residual in 96 us, 5.6 TB/s. Back, each operand is read once
+// too: rows pass through a workgroup that keeps the sums of dw and db of its
+// columns in registers, the next rows' loads ahead of the work on the present
+// ones, and a second launch adds the workgroups' sums: the same rows in 92 us
+// with the sums, 5.8 TB/s.
 #include <algorithm>
 
 #include "ops_device.hpp"
@@ -14,7 +19,6 @@ namespace wb {
 namespace {
 
 constexpr int kMaxWaves = 16;
-constexpr int64_t kManyRows = 2048;
 
 __device__ __forceinline__ float rounded(float v, int type) {
   return type == WB_F32 ? v : __builtin_bit_cast(float, pack_bf16(v, v) << 16);
@@ -30,6 +34,7 @@ __device__ __forceinline__ float sum_of_group(float v, float* part, int waves) {
   for (int w = 0; w < waves; ++w) v += part[w];
   return v;
 }
+
 
 // ---- forward -------------------------------------------------------------------
 // A row takes `waves` wavefronts (ROWS > 1: one, and the workgroup holds ROWS
@@ -196,46 +201,270 @@ __global__ __launch_bounds__(kSlabThreads) void wb_layer_norm_slab_kernel(LayerN
   store_run(to + int64_t(gridDim.x) * a.cols * 4, c, a.cols, WB_F32, db);
 }
 
-// dw and db of the strips' sums: 16 lanes of four columns, 16 groups of strips.
-constexpr int kColumns = 64;
+// Rows that registers hold: a row lies over W wavefronts, V runs of eight columns
+// to a lane, and a workgroup has G of them at a time, whose raw values come while
+// the rows before are worked on. dw and db of a lane's columns stay in registers
+// over the workgroup's rows.
+constexpr int kGradWaves = 8;  // of a workgroup
 
-__global__ __launch_bounds__(256) void wb_layer_norm_columns_kernel(LayerNormGradArgs a, const float* parts, int strips) {
-  __shared__ float sums[16][kColumns];
+template <int TYPE>
+struct Raw;
+template <>
+struct Raw<WB_BF16> {
+  u32x4 v;
+};
+template <>
+struct Raw<WB_F32> {
+  f32x4 v[2];
+};
+
+template <int TYPE, bool NT>
+__device__ __forceinline__ void raw_load(Raw<TYPE>& to, const char* row, uint32_t c) {
+  if constexpr (TYPE == WB_BF16) {
+    to.v = get_u4<NT>(reinterpret_cast<const u32x4_a2*>(row + c * 2u));
+  } else {
+    const auto* p = reinterpret_cast<const f32x4_a4*>(row + c * 4u);
+    to.v[0] = get_f4<NT>(p), to.v[1] = get_f4<NT>(p + 1);
+  }
+}
+
+template <int TYPE>
+__device__ __forceinline__ float raw_get(const Raw<TYPE>& r, int i) {
+  if constexpr (TYPE == WB_BF16)
+    return __builtin_bit_cast(float, (i & 1) ? r.v[i >> 1] & 0xffff0000u : r.v[i >> 1] << 16);
+  else
+    return r.v[i >> 2][i & 3];
+}
+
+template <int TT, int DT, int W, int V, bool NT>
+__global__ __launch_bounds__(64 * kGradWaves) void wb_layer_norm_grad_kernel(LayerNormGradArgs a, float* parts) {
+  constexpr int G = kGradWaves / W;
+  __shared__ float sums[2][kGradWaves][2];
+  extern __shared__ float meet[];  // [2][cols], where G > 1
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = wave / W;
+  const int lane = threadIdx.x - group * (W * 64);
+  const int tb = TT == WB_F32 ? 4 : 2, db = DT == WB_F32 ? 4 : 2;
+  const uint32_t cols = static_cast<uint32_t>(a.cols);
+  // A lane past the row's last whole run has the row's last eight columns: those before its own, `skip` of them, are
+  // another lane's and have a weight of zero here, so that they count once.
+  uint32_t at_col[V];
+  int skip[V];
+  float w[V][8], dw[V][8], sb[V][8];
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    const uint32_t c = (v * (W * 64) + lane) * 8;
+    at_col[v] = min(c, cols - 8);
+    skip[v] = static_cast<int>(min(c - at_col[v], 8u));
+    load_eight(a.weight, at_col[v], a.weight_type, w[v]);
+    for (int i = 0; i < 8; ++i) {
+      if (i < skip[v]) w[v][i] = 0.0f;
+      dw[v][i] = sb[v][i] = 0.0f;
+    }
+  }
+  Raw<TT> t[V], more[V];
+  Raw<DT> d[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) more[v] = Raw<TT>{};
+  const int64_t step = int64_t(gridDim.x) * G, last = a.rows - 1;
+  float mean = 0.0f, inv = 0.0f;
+  const auto fetch = [&](int64_t row) {  // rows past the end read the last one again
+    row = min(row, last);
+    mean = a.mean ? a.mean[row] : 0.0f, inv = a.inv[row];
+    const char *tr = static_cast<const char*>(a.total) + row * a.ld_total * tb, *dr = static_cast<const char*>(a.d_out) + row * a.ld_d_out * db;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      raw_load<TT, NT>(t[v], tr, at_col[v]);
+      raw_load<DT, NT>(d[v], dr, at_col[v]);
+    }
+    if (a.d_total) {
+      const char* mr = static_cast<const char*>(a.d_total) + row * a.ld_d_total * tb;
+#pragma unroll
+      for (int v = 0; v < V; ++v) raw_load<TT, NT>(more[v], mr, at_col[v]);
+    }
+  };
+  const int64_t first = int64_t(blockIdx.x) * G;  // of the workgroup: every group takes as many turns
+  fetch(first + group);
+  const float n = static_cast<float>(a.cols);
+  int turn = 0;
+  for (int64_t at = first; at < a.rows; at += step, turn ^= 1) {
+    const int64_t row = at + group;
+    Raw<TT> tc[V], mc[V];
+    Raw<DT> dc[V];
+    const float mean_now = mean, inv_now = inv;
+#pragma unroll
+    for (int v = 0; v < V; ++v) tc[v] = t[v], mc[v] = more[v], dc[v] = d[v];
+    fetch(row + step);
+    float s1 = 0.0f, s2 = 0.0f;
+    if (row < a.rows) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float dv = raw_get(dc[v], i), h = (raw_get(tc[v], i) - mean_now) * inv_now, g = dv * w[v][i];
+          s1 += g;
+          s2 = __builtin_fmaf(g, h, s2);
+          dw[v][i] = __builtin_fmaf(dv, h, dw[v][i]);
+          sb[v][i] += dv;
+        }
+      }
+    }
+    s1 = sum_of_wave(s1), s2 = sum_of_wave(s2);
+    if (W > 1) {
+      if ((threadIdx.x & 63) == 0) sums[turn][wave][0] = s1, sums[turn][wave][1] = s2;
+      __syncthreads();
+      s1 = s2 = 0.0f;
+#pragma unroll
+      for (int i = 0; i < W; ++i) s1 += sums[turn][group * W + i][0], s2 += sums[turn][group * W + i][1];
+    }
+    if (row >= a.rows) continue;
+    const float m1 = a.mean ? s1 / n : 0.0f, m2 = s2 / n;
+    char* x_row = static_cast<char*>(a.d_x) + row * a.ld_d_x * bytes_of(a.d_x_type);
+    char* r_row = static_cast<char*>(a.d_residual) + row * a.ld_d_residual * bytes_of(a.d_residual_type);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      if (skip[v] == 8) continue;
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float h = (raw_get(tc[v], i) - mean_now) * inv_now;
+        x[i] = __builtin_fmaf(inv_now, __builtin_fmaf(-h, m2, raw_get(dc[v], i) * w[v][i] - m1), raw_get(mc[v], i));
+      }
+      if (skip[v] == 0) {
+        store_eight<NT>(x_row, at_col[v], a.d_x_type, x);
+        if (a.d_residual) store_eight<NT>(r_row, at_col[v], a.d_residual_type, x);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          if (i < skip[v]) continue;
+          store_one(x_row, at_col[v] + i, a.d_x_type, x[i]);
+          if (a.d_residual) store_one(r_row, at_col[v] + i, a.d_residual_type, x[i]);
+        }
+      }
+    }
+  }
+  if (!a.d_weight) return;
+  for (int g = 0; g < G; ++g) {
+    if (g > 0) __syncthreads();
+    if (group != g) continue;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+#pragma unroll
+      for (int which = 0; which < 2; ++which) {
+        float* mine = meet + which * cols + at_col[v];
+        float* out = parts + (int64_t(which) * gridDim.x + blockIdx.x) * cols + at_col[v];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          if (i < skip[v]) continue;
+          float sum = which ? sb[v][i] : dw[v][i];
+          if (g > 0) sum += mine[i];
+          if (g + 1 < G)
+            mine[i] = sum;
+          else
+            out[i] = sum;
+        }
+      }
+    }
+  }
+}
+
+// dw and db of the strips' sums: 16 lanes of four columns, 64 groups of strips.
+constexpr int kColumns = 64, kGroups = 64;
+
+__global__ __launch_bounds__(16 * kGroups) void wb_layer_norm_columns_kernel(LayerNormGradArgs a, const float* parts, int strips) {
+  __shared__ float sums[kGroups][kColumns + 4];
   void* to = blockIdx.y ? a.d_bias : a.d_weight;
-  if (!to) return;
   const int type = blockIdx.y ? a.d_bias_type : a.d_weight_type;
   parts += int64_t(blockIdx.y) * strips * a.cols;
   const int col = (threadIdx.x & 15) * 4, group = threadIdx.x >> 4;
   const int64_t c = int64_t(blockIdx.x) * kColumns + col;
   float sum[4] = {0, 0, 0, 0};
-  for (int s = group; s < strips; s += 16) {
-    const float* from = parts + int64_t(s) * a.cols + c;
-    if (c + 4 <= a.cols) {
-      const f32x4 v = *reinterpret_cast<const f32x4_a4*>(from);
+  if (c + 4 <= a.cols) {
+#pragma unroll 4
+    for (int s = group; s < strips; s += kGroups) {
+      const f32x4 v = *reinterpret_cast<const f32x4_a4*>(parts + int64_t(s) * a.cols + c);
       for (int i = 0; i < 4; ++i) sum[i] += v[i];
-    } else {
-      for (int i = 0; i < 4; ++i)
-        if (c + i < a.cols) sum[i] += from[i];
     }
+  } else {
+    for (int s = group; s < strips; s += kGroups)
+      for (int i = 0; i < 4; ++i)
+        if (c + i < a.cols) sum[i] += parts[int64_t(s) * a.cols + c + i];
   }
   for (int i = 0; i < 4; ++i) sums[group][col + i] = sum[i];
   __syncthreads();
-  const int64_t out = int64_t(blockIdx.x) * kColumns + threadIdx.x;
-  if (threadIdx.x >= kColumns || out >= a.cols) return;
+  if (threadIdx.x >= kColumns * 4) return;
+  // four lanes a column, sixteen groups each
+  const int mine = threadIdx.x >> 2, part = threadIdx.x & 3;
   float all = 0.0f;
-  for (int g = 0; g < 16; ++g) all += sums[g][threadIdx.x];
-  store_one(to, out, type, all);
+  for (int g = 0; g < kGroups / 4; ++g) all += sums[part * (kGroups / 4) + g][mine];
+  all += __shfl_xor(all, 1);
+  all += __shfl_xor(all, 2);
+  const int64_t out = int64_t(blockIdx.x) * kColumns + mine;
+  if (part == 0 && out < a.cols) store_one(to, out, type, all);
 }
 
-int64_t strips_of(int64_t rows, int64_t cols) {
-  const int64_t slabs = (cols + kSlab - 1) / kSlab;
-  return std::max<int64_t>(1, std::min(rows, (2048 + slabs - 1) / slabs));
+// How the gradient's launch goes: strips of rows, each with its sums of dw and
+// db, and wavefronts and runs a row; no wavefronts for rows that registers do
+// not hold, for rows of fewer than eight columns, and for no rows at all, where the
+// kernel above would have none to load.
+struct GradPlan {
+  int64_t strips;
+  int waves, runs;
+};
+
+// One run a lane up to 2048 columns, two above (16384 x 4096 bf16, there and
+// back: 191 us against 215; 1777 x 1501 on an fp32 residual: 31 against 28). A
+// strip per CU: more of them have fewer rows to fetch ahead, and more sums to
+// add (16384 x 4096: 219 us with 512), except narrow rows, of which two
+// workgroups fit a CU (16384 x 2048: 106 us with 512, 114 with 256).
+GradPlan grad_plan(int64_t rows, int64_t cols) {
+  GradPlan p{};
+  p.runs = cols <= 2048 ? 1 : 2;
+  p.waves = 1;
+  while (p.waves * 64 * 8 * p.runs < cols) p.waves *= 2;
+  if (p.waves > kGradWaves || cols < 8 || rows == 0) {
+    const int64_t slabs = (cols + kSlab - 1) / kSlab;
+    p.waves = 0;
+    p.strips = std::max<int64_t>(1, std::min(rows, (2048 + slabs - 1) / slabs));
+    return p;
+  }
+  const int64_t groups = kGradWaves / p.waves;
+  p.strips = std::min<int64_t>((rows + groups - 1) / groups, p.runs == 1 && rows >= 8192 ? 512 : 256);
+  p.strips = std::max<int64_t>(1, p.strips);
+  return p;
+}
+
+template <int TT, int DT, int W, int V>
+hipError_t launch_grad(const LayerNormGradArgs& a, const GradPlan& p, float* parts, hipStream_t st) {
+  const int64_t row_bytes = a.cols * (bytes_of(TT) * (a.d_total ? 2 : 1) + bytes_of(DT) + bytes_of(a.d_x_type) +
+                                      (a.d_residual ? bytes_of(a.d_residual_type) : 0));
+  const size_t lds = kGradWaves > W && a.d_weight ? a.cols * 8 : 0;
+  const auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>(p.strips)), dim3(64 * kGradWaves), lds, st, a, parts);
+    return hipGetLastError();
+  };
+  return a.rows * row_bytes > kStreamBytes ? go(wb_layer_norm_grad_kernel<TT, DT, W, V, true>)
+                                           : go(wb_layer_norm_grad_kernel<TT, DT, W, V, false>);
+}
+
+template <int TT, int DT, int V>
+hipError_t by_waves(const LayerNormGradArgs& a, const GradPlan& p, float* parts, hipStream_t st) {
+  switch (p.waves) {
+    case 1: return launch_grad<TT, DT, 1, V>(a, p, parts, st);
+    case 2: return launch_grad<TT, DT, 2, V>(a, p, parts, st);
+    case 4: return launch_grad<TT, DT, 4, V>(a, p, parts, st);
+    default: return launch_grad<TT, DT, 8, V>(a, p, parts, st);
+  }
+}
+
+template <int TT, int DT>
+hipError_t by_runs(const LayerNormGradArgs& a, const GradPlan& p, float* parts, hipStream_t st) {
+  return p.runs == 1 ? by_waves<TT, DT, 1>(a, p, parts, st) : by_waves<TT, DT, 2>(a, p, parts, st);
 }
 
 }  // namespace
 
 size_t layer_norm_grad_workspace_bytes(int64_t rows, int64_t cols) {
-  return static_cast<size_t>((rows * 2 + 2 * strips_of(rows, cols) * cols) * 4);
+  return static_cast<size_t>((rows * 2 + 2 * grad_plan(rows, cols).strips * cols) * 4);
 }
 
 int launch_layer_norm(const LayerNormArgs& a, void* stream) {
@@ -243,10 +472,13 @@ int launch_layer_norm(const LayerNormArgs& a, void* stream) {
   if (a.rows == 0) return hipSuccess;
   const int64_t runs = (a.cols + 7) / 8;
   const auto waves = [&](int v) { return static_cast<int>((runs + 64 * v - 1) / (64 * v)); };
+  // Narrow rows: one wavefront each, four to a workgroup. Wider ones: two runs
+  // a lane (16384 x 4096 bf16 with a residual: 96 us against 115 of one, 105 of
+  // four and 123 of a wavefront a row; 512 x 7168: 9.0 us against 11.0 and 10.7),
+  // past sixteen wavefronts four, past those several steps.
   if (runs <= 64) return launch<1, 4, false>(a, 1, st);
   if (runs <= 128) return launch<2, 4, false>(a, 1, st);
-  if (a.rows >= kManyRows && runs <= 512) return launch<1, 1, false>(a, waves(1), st);
-  if (a.rows < kManyRows && waves(2) <= kMaxWaves) return launch<2, 1, false>(a, waves(2), st);
+  if (waves(2) <= kMaxWaves) return launch<2, 1, false>(a, waves(2), st);
   if (waves(4) <= kMaxWaves) return launch<4, 1, false>(a, waves(4), st);
   return launch<4, 1, true>(a, kMaxWaves, st);
 }
@@ -254,22 +486,30 @@ int launch_layer_norm(const LayerNormArgs& a, void* stream) {
 int launch_layer_norm_grad(const LayerNormGradArgs& a, void* stream) {
   const auto st = static_cast<hipStream_t>(stream);
   float *sums = a.workspace, *parts = a.workspace + a.rows * 2;
-  const int64_t strips = strips_of(a.rows, a.cols);
-  if (a.rows > 0) {
-    const int64_t runs = (a.cols + 7) / 8;
-    const int waves = static_cast<int>(std::min<int64_t>(kMaxWaves, (runs + 63) / 64));
-    hipLaunchKernelGGL(wb_layer_norm_sums_kernel, dim3(static_cast<uint32_t>(a.rows)), dim3(64 * waves), 0, st, a, sums);
+  const GradPlan p = grad_plan(a.rows, a.cols);
+  if (p.waves == 0 || (a.d_total && a.d_total_type != a.total_type)) {
+    if (a.rows > 0) {
+      const int64_t runs = (a.cols + 7) / 8;
+      const int waves = static_cast<int>(std::min<int64_t>(kMaxWaves, (runs + 63) / 64));
+      hipLaunchKernelGGL(wb_layer_norm_sums_kernel, dim3(static_cast<uint32_t>(a.rows)), dim3(64 * waves), 0, st, a, sums);
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(wb_layer_norm_slab_kernel,
+                       dim3(static_cast<uint32_t>(p.strips), static_cast<uint32_t>((a.cols + kSlab - 1) / kSlab)),
+                       dim3(kSlabThreads), 0, st, a, sums, parts);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
+  } else {
+    const bool t32 = a.total_type == WB_F32, d32 = a.d_out_type == WB_F32;
+    const hipError_t e = t32 ? (d32 ? by_runs<WB_F32, WB_F32>(a, p, parts, st) : by_runs<WB_F32, WB_BF16>(a, p, parts, st))
+                             : (d32 ? by_runs<WB_BF16, WB_F32>(a, p, parts, st) : by_runs<WB_BF16, WB_BF16>(a, p, parts, st));
+    if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(wb_layer_norm_slab_kernel,
-                     dim3(static_cast<uint32_t>(strips), static_cast<uint32_t>((a.cols + kSlab - 1) / kSlab)),
-                     dim3(kSlabThreads), 0, st, a, sums, parts);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !a.d_weight) return e;
+  if (!a.d_weight) return hipSuccess;
   hipLaunchKernelGGL(wb_layer_norm_columns_kernel,
-                     dim3(static_cast<uint32_t>((a.cols + kColumns - 1) / kColumns), a.d_bias ? 2 : 1), dim3(256), 0, st, a,
-                     parts, static_cast<int>(strips));
+                     dim3(static_cast<uint32_t>((a.cols + kColumns - 1) / kColumns), a.d_bias ? 2 : 1), dim3(16 * kGroups), 0, st,
+                     a, parts, static_cast<int>(p.strips));
   return hipGetLastError();
 }
 
