@@ -59,7 +59,7 @@ __global__ __launch_bounds__(kThreads) void wb_embed_kernel(EmbedArgs a, int shi
 // the digits' counts, then places.
 
 constexpr int kOneBlock = 8192, kOneThreads = 1024;
-constexpr int kSortThreads = 256, kSortItems = 8, kSortTile = kSortThreads * kSortItems, kMaxSortBlocks = 256;
+constexpr int kSortThreads = 256, kSortItems = 8, kMaxSortBlocks = 256;
 constexpr int kMaxDigits = 512;
 
 struct Passes {
@@ -75,7 +75,8 @@ Passes passes_of(int64_t rows) {  // keys 0..rows
 
 int64_t sort_block(int64_t count) {
   const int64_t per = (count + kMaxSortBlocks - 1) / kMaxSortBlocks;
-  return (per + kSortTile - 1) / kSortTile * kSortTile;
+  const int64_t tile = kSortThreads * (per >= kSortThreads * kSortItems ? kSortItems : 1);
+  return (per + tile - 1) / tile * tile;
 }
 
 // The lanes below this one, and all, that hold the same digit.
@@ -187,7 +188,7 @@ __global__ __launch_bounds__(kOneThreads) void wb_sort_few_kernel(EmbedGradArgs 
   }
 }
 
-// Counts of a pass's digits by block, table[digit][block]. FIRST: the keys are
+// Counts of a pass's digits by block, table[block][digit]. FIRST: the keys are
 // made from the tokens.
 template <bool FIRST>
 __global__ __launch_bounds__(kSortThreads) void wb_sort_count_kernel(EmbedGradArgs a, const uint32_t* keys, uint32_t* table,
@@ -202,10 +203,11 @@ __global__ __launch_bounds__(kSortThreads) void wb_sort_count_kernel(EmbedGradAr
     atomicAdd(&counts[(key >> shift) & (digits - 1)], 1u);
   }
   __syncthreads();
-  for (int d = threadIdx.x; d < digits; d += kSortThreads) table[int64_t(d) * gridDim.x + blockIdx.x] = counts[d];
+  for (int d = threadIdx.x; d < digits; d += kSortThreads) table[blockIdx.x * digits + d] = counts[d];
 }
 
-template <bool FIRST>
+// ITEMS: tokens of a thread at a time; one where there are few, for more blocks.
+template <bool FIRST, int ITEMS>
 __global__ __launch_bounds__(kSortThreads) void wb_sort_place_kernel(EmbedGradArgs a, const uint32_t* keys,
                                                                      const int32_t* order, const uint32_t* table,
                                                                      uint32_t* keys_to, int32_t* order_to, int64_t per,
@@ -217,8 +219,9 @@ __global__ __launch_bounds__(kSortThreads) void wb_sort_place_kernel(EmbedGradAr
   // a digit's first place: those of the smaller digits, and of this one in the blocks before
   for (int d = tid; d < digits; d += kSortThreads) {
     uint32_t all = 0, before = 0;
+#pragma unroll 32
     for (int b = 0; b < blocks; ++b) {
-      const uint32_t c = table[int64_t(d) * blocks + b];
+      const uint32_t c = table[b * digits + d];
       all += c;
       before += b < int(blockIdx.x) ? c : 0;
     }
@@ -230,21 +233,21 @@ __global__ __launch_bounds__(kSortThreads) void wb_sort_place_kernel(EmbedGradAr
   for (int d = tid; d < digits; d += kSortThreads) next[d] += mine[d];
   __syncthreads();
   const int64_t begin = int64_t(blockIdx.x) * per, end = min(begin + per, a.count);
-  for (int64_t tile = begin; tile < end; tile += kSortTile) {
+  for (int64_t tile = begin; tile < end; tile += kSortThreads * ITEMS) {
     for (int d = tid; d < kWaves * digits; d += kSortThreads) seen[d >> bits][d & (digits - 1)] = 0;
     __syncthreads();
-    uint32_t key[kSortItems], rank[kSortItems];
-    int32_t from[kSortItems];
+    uint32_t key[ITEMS], rank[ITEMS];
+    int32_t from[ITEMS];
 #pragma unroll
-    for (int i = 0; i < kSortItems; ++i) {
-      const int64_t t = tile + (wave * kSortItems + i) * 64 + lane;
+    for (int i = 0; i < ITEMS; ++i) {
+      const int64_t t = tile + (wave * ITEMS + i) * 64 + lane;
       if (t >= end) continue;
       key[i] = FIRST ? row_of(a.tokens, a.token_bytes, t, a.first, a.rows) : keys[t];
       from[i] = FIRST ? static_cast<int32_t>(t) : order[t];
     }
 #pragma unroll
-    for (int i = 0; i < kSortItems; ++i) {
-      const bool on = tile + (wave * kSortItems + i) * 64 + lane < end;
+    for (int i = 0; i < ITEMS; ++i) {
+      const bool on = tile + (wave * ITEMS + i) * 64 + lane < end;
       const uint32_t digit = on ? (key[i] >> shift) & (digits - 1) : 0;
       const uint64_t same = same_digit(digit, bits, on);
       const uint32_t before = seen[wave][digit];
@@ -265,8 +268,8 @@ __global__ __launch_bounds__(kSortThreads) void wb_sort_place_kernel(EmbedGradAr
     }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kSortItems; ++i) {
-      if (tile + (wave * kSortItems + i) * 64 + lane >= end) continue;
+    for (int i = 0; i < ITEMS; ++i) {
+      if (tile + (wave * ITEMS + i) * 64 + lane >= end) continue;
       const uint32_t digit = (key[i] >> shift) & (digits - 1);
       const uint32_t to = next[digit] + seen[wave][digit] + rank[i];
       keys_to[to] = key[i];
@@ -279,100 +282,164 @@ __global__ __launch_bounds__(kSortThreads) void wb_sort_place_kernel(EmbedGradAr
 }
 
 // ---- sums --------------------------------------------------------------------
-// Sorted tokens are taken in chunks of kChunk. A run of equal tokens inside one
-// chunk is summed and written; one that goes over an end leaves an fp32 row
-// per chunk (0: the run that came in, 1: the one that goes on), which the second launch adds.
+// Sorted tokens are taken in chunks. A run of equal tokens inside one chunk is
+// summed and written; one that goes over an end leaves an fp32 row per chunk (0:
+// the run that came in, 1: the one that goes on), which the second launch adds.
 
-constexpr int kChunk = 32;
 constexpr int kFillRows = 32;
+constexpr int kBatch = 8;  // rows under way at a time
 
 struct Sorted {
   const uint32_t* keys;
   const int32_t* order;
   float* partial;  // [chunks][2][cols]
   int64_t chunks;
+  int32_t chunk;  // tokens of one
 };
 
+template <bool NT = false>
 __device__ __forceinline__ void store_scaled(const EmbedGradArgs& a, uint32_t v, int64_t c, float (&sum)[8]) {
   char* to = static_cast<char*>(a.d_weight) + int64_t(v) * a.ld_d_weight * bytes_of(a.d_weight_type);
   for (int j = 0; j < 8; ++j) sum[j] *= a.scale;
-  store_run(to, c, a.cols, a.d_weight_type, sum);
+  store_run<NT>(to, c, a.cols, a.d_weight_type, sum);
 }
 
-__global__ __launch_bounds__(kThreads) void wb_embed_sum_kernel(EmbedGradArgs a, Sorted s, int shift, int64_t chunk_blocks) {
-  const int lanes = 1 << shift, lane = threadIdx.x & (lanes - 1), sub = threadIdx.x >> shift, per = kThreads >> shift;
-  if (int64_t(blockIdx.x) >= chunk_blocks) {  // rows without a token
-    __shared__ uint32_t start[kFillRows + 1];
-    const int64_t v0 = (int64_t(blockIdx.x) - chunk_blocks) * kFillRows;
-    if (threadIdx.x <= kFillRows) {  // the first place of a key not below v0 + threadIdx.x
-      int64_t lo = 0, hi = a.count;
-      while (lo < hi) {
-        const int64_t mid = (lo + hi) >> 1;
-        if (s.keys[mid] < v0 + threadIdx.x)
-          lo = mid + 1;
-        else
-          hi = mid;
-      }
-      start[threadIdx.x] = static_cast<uint32_t>(lo);
+// The first place of a key not below v, by all lanes of a wavefront: 64 places
+// are looked at in a step, which takes three for 2^18 tokens where halves take
+// eighteen, each a trip to memory.
+__device__ __forceinline__ int64_t first_not_below(const uint32_t* keys, int64_t count, uint64_t v) {
+  int64_t lo = 0, hi = count;  // keys before lo are below v, from hi on they are not
+  while (lo < hi) {
+    const int64_t step = (hi - lo + 63) >> 6, at = lo + (threadIdx.x & 63) * step;
+    const int below = __popcll(__ballot(at < hi && keys[min(at, hi - 1)] < v));
+    if (below == 0) break;
+    hi = min(hi, lo + below * step);
+    lo += (below - 1) * step + 1;
+  }
+  return lo;
+}
+
+// Zeros into the rows of a workgroup that no token names.
+template <bool NT>
+__device__ __forceinline__ void fill_rows(const EmbedGradArgs& a, const Sorted& s, int64_t v0, int shift) {
+  __shared__ int named[kFillRows];
+  if (threadIdx.x < kFillRows) named[threadIdx.x] = 0;
+  __syncthreads();
+  const int64_t at = first_not_below(s.keys, a.count, v0) + threadIdx.x;
+  const uint32_t key = at < a.count ? s.keys[at] : ~0u;
+  const bool mine = key < v0 + kFillRows;
+  if (mine) named[key - v0] = 1;
+  if (__syncthreads_and(mine)) {  // their tokens go on past the workgroup's threads
+    for (int r = threadIdx.x >> 6; r < kFillRows; r += kThreads / 64) {
+      const int64_t first = first_not_below(s.keys, a.count, v0 + r);
+      if ((threadIdx.x & 63) == 0) named[r] = first < a.count && s.keys[first] == v0 + r;
     }
     __syncthreads();
-    const float none[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    for (int r = sub; r < kFillRows; r += per) {
-      const int64_t v = v0 + r;
-      if (v >= a.rows || start[r] != start[r + 1]) continue;
-      char* to = static_cast<char*>(a.d_weight) + v * a.ld_d_weight * bytes_of(a.d_weight_type);
-      for (int64_t c = (int64_t(blockIdx.y) * lanes + lane) * 8; c < a.cols; c += int64_t(gridDim.y) * lanes * 8) {
-        store_run(to, c, a.cols, a.d_weight_type, none);
-      }
-    }
-    return;
   }
-  const int64_t chunk = int64_t(blockIdx.x) * per + sub;
-  const int64_t c = (int64_t(blockIdx.y) * lanes + lane) * 8;
-  if (chunk >= s.chunks || c >= a.cols) return;
-  const int64_t begin = chunk * kChunk, end = min(begin + kChunk, a.count);
-  const int db = a.d_out_type == WB_F32 ? 4 : 2;
-  float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-  bool came = begin > 0 && s.keys[begin - 1] == s.keys[begin];  // the run began before this chunk
-  for (int64_t p = begin; p < end; ++p) {
-    const uint32_t v = s.keys[p];
-    if (v >= a.rows) break;  // tokens of other rows, sorted last
-    const char* row = static_cast<const char*>(a.d_out) + int64_t(s.order[p]) * a.ld_d_out * db;
-    float x[8];
-    load_run(row, c, a.cols, a.d_out_type, x);
-    for (int j = 0; j < 8; ++j) sum[j] += x[j];
-    const bool on = p + 1 < a.count && s.keys[p + 1] == v;
-    if (on && p + 1 < end) continue;
-    if (came || on) {
-      store_run(reinterpret_cast<char*>(s.partial + (chunk * 2 + (came ? 0 : 1)) * a.cols), c, a.cols, WB_F32, sum);
-    } else {
-      store_scaled(a, v, c, sum);
-    }
-    for (int j = 0; j < 8; ++j) sum[j] = 0.0f;
-    came = false;
+  const int lanes = 1 << shift, lane = threadIdx.x & (lanes - 1);
+  const float none[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  for (int r = threadIdx.x >> shift; r < kFillRows; r += kThreads >> shift) {
+    const int64_t v = v0 + r;
+    if (v >= a.rows || named[r]) continue;
+    char* to = static_cast<char*>(a.d_weight) + v * a.ld_d_weight * bytes_of(a.d_weight_type);
+    for (int64_t c = lane * 8; c < a.cols; c += lanes * 8) store_run<NT>(to, c, a.cols, a.d_weight_type, none);
   }
 }
 
-// The runs that go over the end of the chunk they began in.
-__global__ __launch_bounds__(kThreads) void wb_embed_join_kernel(EmbedGradArgs a, Sorted s, int shift) {
+template <bool NT>
+__global__ __launch_bounds__(kThreads) void wb_embed_sum_kernel(EmbedGradArgs a, Sorted s, int shift, int64_t sums, uint32_t slabs) {
+  if (int64_t(blockIdx.x) >= sums) {
+    fill_rows<NT>(a, s, (int64_t(blockIdx.x) - sums) * kFillRows, shift);
+    return;
+  }
   const int lanes = 1 << shift, lane = threadIdx.x & (lanes - 1);
-  const int64_t chunk = int64_t(blockIdx.x) * (kThreads >> shift) + (threadIdx.x >> shift);
-  const int64_t c = (int64_t(blockIdx.y) * lanes + lane) * 8;
-  if (chunk + 1 >= s.chunks || c >= a.cols) return;
-  const int64_t begin = chunk * kChunk, end = begin + kChunk;
+  const uint32_t block = blockIdx.x / slabs, slab = blockIdx.x - block * slabs;
+  const int64_t chunk = int64_t(block) * (kThreads >> shift) + (threadIdx.x >> shift);
+  if (chunk >= s.chunks) return;
+  const int64_t c = (int64_t(slab) * lanes + lane) * 8;
+  const int64_t begin = chunk * s.chunk, end = min(begin + s.chunk, a.count);
+  const int db = a.d_out_type == WB_F32 ? 4 : 2;
+  const int here = threadIdx.x & 63 & ~(lanes - 1);  // the wavefront's lane with this chunk's first token
+  float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  bool came = begin > 0 && s.keys[begin - 1] == s.keys[begin];  // the run began before this chunk
+  for (int64_t base = begin; base < end; base += kBatch) {
+    // eight lanes have the batch's tokens and the ones after them
+    const int64_t mine = min(base + (lane & (kBatch - 1)), end - 1);
+    const uint32_t key = s.keys[mine], then = mine + 1 < a.count ? s.keys[mine + 1] : ~0u;
+    const int32_t from = s.order[mine];
+    const int n = static_cast<int>(min(int64_t(kBatch), end - base));
+    float x[kBatch][8];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const char* row = static_cast<const char*>(a.d_out) + int64_t(__shfl(from, here + i)) * a.ld_d_out * db;
+      if (c < a.cols) load_run<NT>(row, c, a.cols, a.d_out_type, x[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const uint32_t v = __shfl(key, here + i), next = __shfl(then, here + i);
+      if (i >= n || v >= a.rows) continue;  // tokens of other rows are sorted last
+      for (int j = 0; j < 8; ++j) sum[j] += x[i][j];
+      const bool on = next == v;
+      if (on && base + i + 1 < end) continue;
+      if (c < a.cols) {
+        if (came || on)
+          store_run(reinterpret_cast<char*>(s.partial + (chunk * 2 + (came ? 0 : 1)) * a.cols), c, a.cols, WB_F32, sum);
+        else
+          store_scaled<NT>(a, v, c, sum);
+      }
+      for (int j = 0; j < 8; ++j) sum[j] = 0.0f;
+      came = false;
+    }
+  }
+}
+
+// The runs that go over the end of the chunk they began in: a workgroup for
+// each chunk's last run and 512 columns, its wavefronts over the chunks that the
+// run goes on in.
+constexpr int kJoinColumns = 512;
+
+__global__ __launch_bounds__(kThreads) void wb_embed_join_kernel(EmbedGradArgs a, Sorted s) {
+  constexpr int kWaves = kThreads / 64;
+  __shared__ float meet[kWaves][kJoinColumns];
+  const int64_t chunk = blockIdx.x, begin = chunk * s.chunk, end = begin + s.chunk;
   const uint32_t v = s.keys[end - 1];
   if (v >= a.rows || s.keys[end] != v) return;
   if (s.keys[begin] == v && begin > 0 && s.keys[begin - 1] == v) return;  // it began before
-  float sum[8], x[8];
-  auto load = [&](int64_t slot, float(&to)[8]) {
-    load_run(reinterpret_cast<const char*>(s.partial + slot * a.cols), c, a.cols, WB_F32, to);
-  };
-  load(chunk * 2 + 1, sum);
-  for (int64_t next = chunk + 1; next < s.chunks && s.keys[next * kChunk] == v; ++next) {
-    load(next * 2, x);
-    for (int j = 0; j < 8; ++j) sum[j] += x[j];
+  // chunks that go on: all up to the first that begins with another token
+  int64_t last = chunk + 1;
+  for (bool all = true; all; last += kThreads) {
+    const int64_t at = last + threadIdx.x;
+    const bool on = at < s.chunks && s.keys[at * s.chunk] == v;
+    all = __syncthreads_and(on);
+    if (!all) {
+      last += __syncthreads_count(on) - kThreads;
+    }
   }
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int64_t c = int64_t(blockIdx.y) * kJoinColumns + lane * 8;
+  float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  if (c < a.cols) {
+    if (wave == 0) load_run(reinterpret_cast<const char*>(s.partial + (chunk * 2 + 1) * a.cols), c, a.cols, WB_F32, sum);
+#pragma unroll 4
+    for (int64_t next = chunk + 1 + wave; next < last; next += kWaves) {
+      float x[8];
+      load_run(reinterpret_cast<const char*>(s.partial + next * 2 * a.cols), c, a.cols, WB_F32, x);
+      for (int j = 0; j < 8; ++j) sum[j] += x[j];
+    }
+  }
+  for (int j = 0; j < 8; ++j) meet[wave][lane * 8 + j] = sum[j];
+  __syncthreads();
+  if (wave > 0 || c >= a.cols) return;
+  for (int w = 1; w < kWaves; ++w)
+    for (int j = 0; j < 8; ++j) sum[j] += meet[w][lane * 8 + j];
   store_scaled(a, v, c, sum);
+}
+
+// Short chunks give few tokens more workgroups, long ones leave many tokens' runs fewer rows to add.
+int chunk_of(int64_t count) {
+  int chunk = 32;
+  while (chunk < 256 && count > int64_t(chunk) * 1024) chunk *= 2;
+  return chunk;
 }
 
 int64_t up16(int64_t n) { return (n + 15) / 16 * 16; }
@@ -393,7 +460,8 @@ Layout layout_of(int64_t count, int64_t rows, int64_t cols) {
   const bool few = count <= kOneBlock;
   for (int i = 0; i < (few ? 1 : 2); ++i) l.keys[i] = take(count * 4), l.order[i] = take(count * 4);
   if (!few) l.table = take((int64_t(4) << passes_of(rows).bits) * kMaxSortBlocks);
-  l.partial = take(count > kChunk ? (count + kChunk - 1) / kChunk * 2 * cols * 4 : 0);
+  const int64_t chunk = chunk_of(count);
+  l.partial = take(count > chunk ? (count + chunk - 1) / chunk * 2 * cols * 4 : 0);
   l.all = at;
   return l;
 }
@@ -438,15 +506,16 @@ int launch_embed_grad(const EmbedGradArgs& a, void* stream) {
     auto* table = reinterpret_cast<uint32_t*>(ws + l.table);
     for (int i = 0; i < p.count; ++i) {
       const int from = now, to = i == 0 ? 0 : 1 - now, shift = i * p.bits;
-      if (i == 0) {
-        hipLaunchKernelGGL(wb_sort_count_kernel<true>, grid, dim3(kSortThreads), 0, st, a, nullptr, table, per, shift, p.bits);
-        hipLaunchKernelGGL(wb_sort_place_kernel<true>, grid, dim3(kSortThreads), 0, st, a, nullptr, nullptr, table, keys(to),
-                           order(to), per, shift, p.bits);
-      } else {
-        hipLaunchKernelGGL(wb_sort_count_kernel<false>, grid, dim3(kSortThreads), 0, st, a, keys(from), table, per, shift, p.bits);
-        hipLaunchKernelGGL(wb_sort_place_kernel<false>, grid, dim3(kSortThreads), 0, st, a, keys(from), order(from), table,
-                           keys(to), order(to), per, shift, p.bits);
-      }
+      const auto pass = [&](auto counts, auto places) {
+        hipLaunchKernelGGL(counts, grid, dim3(kSortThreads), 0, st, a, keys(from), table, per, shift, p.bits);
+        hipLaunchKernelGGL(places, grid, dim3(kSortThreads), 0, st, a, keys(from), order(from), table, keys(to), order(to), per,
+                           shift, p.bits);
+      };
+      const bool many = per % (kSortThreads * kSortItems) == 0;
+      if (i == 0)
+        pass(wb_sort_count_kernel<true>, many ? wb_sort_place_kernel<true, kSortItems> : wb_sort_place_kernel<true, 1>);
+      else
+        pass(wb_sort_count_kernel<false>, many ? wb_sort_place_kernel<false, kSortItems> : wb_sort_place_kernel<false, 1>);
       const hipError_t e = hipGetLastError();
       if (e != hipSuccess) return e;
       now = to;
@@ -454,17 +523,19 @@ int launch_embed_grad(const EmbedGradArgs& a, void* stream) {
   }
   Sorted s{};
   s.keys = keys(now), s.order = order(now), s.partial = reinterpret_cast<float*>(ws + l.partial);
-  s.chunks = (a.count + kChunk - 1) / kChunk;
+  s.chunk = chunk_of(a.count);
+  s.chunks = (a.count + s.chunk - 1) / s.chunk;
   const int shift = row_shift(a.cols);
-  const int64_t per = kThreads >> shift, slab = int64_t(8) << shift;
-  const int64_t blocks = (s.chunks + per - 1) / per, fills = (a.rows + kFillRows - 1) / kFillRows;
-  const uint32_t slabs = static_cast<uint32_t>((a.cols + slab - 1) / slab);
-  if (blocks + fills == 0) return hipSuccess;
-  hipLaunchKernelGGL(wb_embed_sum_kernel, dim3(static_cast<uint32_t>(blocks + fills), slabs), dim3(kThreads), 0, st, a, s, shift,
-                     blocks);
-  hipError_t e = hipGetLastError();
+  const int64_t per = kThreads >> shift, slabs = (a.cols + (int64_t(8) << shift) - 1) / (int64_t(8) << shift);
+  const int64_t sums = (s.chunks + per - 1) / per * slabs, fills = (a.rows + kFillRows - 1) / kFillRows;
+  if (sums + fills == 0) return hipSuccess;
+  const bool nt = a.cols * (a.rows * bytes_of(a.d_weight_type) + a.count * bytes_of(a.d_out_type)) > kStreamBytes;
+  hipLaunchKernelGGL(nt ? wb_embed_sum_kernel<true> : wb_embed_sum_kernel<false>, dim3(static_cast<uint32_t>(sums + fills)),
+                     dim3(kThreads), 0, st, a, s, shift, sums, static_cast<uint32_t>(slabs));
+  const hipError_t e = hipGetLastError();
   if (e != hipSuccess || s.chunks < 2) return e;
-  hipLaunchKernelGGL(wb_embed_join_kernel, dim3(static_cast<uint32_t>(blocks), slabs), dim3(kThreads), 0, st, a, s, shift);
+  hipLaunchKernelGGL(wb_embed_join_kernel, dim3(static_cast<uint32_t>(s.chunks - 1), static_cast<uint32_t>((a.cols + kJoinColumns - 1) / kJoinColumns)),
+                     dim3(kThreads), 0, st, a, s);
   return hipGetLastError();
 }
 

@@ -37,7 +37,7 @@ def draw_tokens(shape, vocab, seed, kind=torch.int64, extra=0.0):
 # ---- embeddings --------------------------------------------------------------------------------
 
 EMBED = [(1, 1, 1), (1, 7, 8), (3, 5, 64), (0, 9, 16), (40, 3, 129), (100, 1000, 72), (33, 2, 2049), (65, 40, 4100),
-         (1000, 300, 513), (31, 513, 8), (32, 600, 40), (8192, 700, 24), (8193, 700, 24), (20000, 262200, 8), (70000, 37, 16)]
+         (1000, 300, 513), (31, 513, 8), (32, 600, 40), (8192, 700, 24), (8193, 700, 24), (20000, 262200, 8), (70000, 37, 16), (530000, 1000, 8)]
 
 
 @pytest.mark.parametrize("shape", EMBED, ids=lambda s: "x".join(map(str, s)))
