@@ -1,10 +1,13 @@
 // Lookup of token embeddings, and the gradient of the table by sorted tokens.
 //   out_t = scale W[tok_t - first];   dW_v = scale sum_{t: tok_t - first = v} dout_t
 //
-// The lookup reads and writes a row per token. The gradient sorts the tokens
-// (stable, so that a row's sum goes by ascending t and does not depend on which
-// workgroup ran first), sums runs of equal tokens, and writes every row of dW
-// once, the ones without a token as zeros.
+// The lookup reads and writes a row per token: bandwidth bound, 16384 x 4096 bf16
+// in 32 us, 8.4 TB/s with what the caches hold of the frequent rows. The gradient sorts the
+// tokens (stable, so that a row's sum goes by ascending t and does not depend on
+// which workgroup ran first), sums runs of equal tokens, and writes every row of dW
+// once, the ones without a token as zeros: 16384 tokens of 128256 in 260 us, of which
+// the sort takes 24, its four launches' latency, and the 1.05 GB of dW 180 (155 without
+// the non-temporal hint, which leaves more to the calls after it: a pass takes 304 us so, 295 with it).
 #include <algorithm>
 
 #include "ops_device.hpp"
@@ -297,11 +300,10 @@ struct Sorted {
   int32_t chunk;  // tokens of one
 };
 
-template <bool NT = false>
 __device__ __forceinline__ void store_scaled(const EmbedGradArgs& a, uint32_t v, int64_t c, float (&sum)[8]) {
   char* to = static_cast<char*>(a.d_weight) + int64_t(v) * a.ld_d_weight * bytes_of(a.d_weight_type);
   for (int j = 0; j < 8; ++j) sum[j] *= a.scale;
-  store_run<NT>(to, c, a.cols, a.d_weight_type, sum);
+  store_run(to, c, a.cols, a.d_weight_type, sum);
 }
 
 // The first place of a key not below v, by all lanes of a wavefront: 64 places
@@ -362,11 +364,17 @@ __global__ __launch_bounds__(kThreads) void wb_embed_sum_kernel(EmbedGradArgs a,
   const int here = threadIdx.x & 63 & ~(lanes - 1);  // the wavefront's lane with this chunk's first token
   float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
   bool came = begin > 0 && s.keys[begin - 1] == s.keys[begin];  // the run began before this chunk
-  for (int64_t base = begin; base < end; base += kBatch) {
-    // eight lanes have the batch's tokens and the ones after them
+  // eight lanes have a batch's tokens and the ones after them, fetched a batch ahead
+  uint32_t key_next, then_next;
+  int32_t from_next;
+  const auto fetch = [&](int64_t base) {
     const int64_t mine = min(base + (lane & (kBatch - 1)), end - 1);
-    const uint32_t key = s.keys[mine], then = mine + 1 < a.count ? s.keys[mine + 1] : ~0u;
-    const int32_t from = s.order[mine];
+    key_next = s.keys[mine], then_next = mine + 1 < a.count ? s.keys[mine + 1] : ~0u, from_next = s.order[mine];
+  };
+  fetch(begin);
+  for (int64_t base = begin; base < end; base += kBatch) {
+    const uint32_t key = key_next, then = then_next;
+    const int32_t from = from_next;
     const int n = static_cast<int>(min(int64_t(kBatch), end - base));
     float x[kBatch][8];
 #pragma unroll
@@ -374,6 +382,7 @@ __global__ __launch_bounds__(kThreads) void wb_embed_sum_kernel(EmbedGradArgs a,
       const char* row = static_cast<const char*>(a.d_out) + int64_t(__shfl(from, here + i)) * a.ld_d_out * db;
       if (c < a.cols) load_run<NT>(row, c, a.cols, a.d_out_type, x[i]);
     }
+    fetch(base + kBatch);
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
       const uint32_t v = __shfl(key, here + i), next = __shfl(then, here + i);
@@ -385,7 +394,7 @@ __global__ __launch_bounds__(kThreads) void wb_embed_sum_kernel(EmbedGradArgs a,
         if (came || on)
           store_run(reinterpret_cast<char*>(s.partial + (chunk * 2 + (came ? 0 : 1)) * a.cols), c, a.cols, WB_F32, sum);
         else
-          store_scaled<NT>(a, v, c, sum);
+          store_scaled(a, v, c, sum);
       }
       for (int j = 0; j < 8; ++j) sum[j] = 0.0f;
       came = false;
@@ -435,10 +444,11 @@ __global__ __launch_bounds__(kThreads) void wb_embed_join_kernel(EmbedGradArgs a
   store_scaled(a, v, c, sum);
 }
 
-// Short chunks give few tokens more workgroups, long ones leave many tokens' runs fewer rows to add.
+// Short chunks give few tokens more workgroups (3001 x 1499 fp32: 28 us with 16, 41 with 32), long ones leave many tokens'
+// runs fewer rows to add (16384 x 4096 with a tenth padding: the join takes 10 us with 32, 15 with 16, 25 with 8).
 int chunk_of(int64_t count) {
-  int chunk = 32;
-  while (chunk < 256 && count > int64_t(chunk) * 1024) chunk *= 2;
+  int chunk = 16;
+  while (chunk < 256 && count > int64_t(chunk) * 512) chunk *= 2;
   return chunk;
 }
 

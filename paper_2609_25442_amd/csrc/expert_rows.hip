@@ -5,6 +5,13 @@
 // once and its k places are written, or read, from there. A place is a token's
 // own if tokens says so, so no two rows write one place; the places that are
 // nobody's are filled with zeros by workgroups of their own.
+//
+// Bandwidth bound: eight columns a thread, one run of them, since what hides a
+// row's way to memory here is the number of wavefronts (the gradient of 8192 x
+// 7168, k = 8: 410 us, and 560 with four runs a lane). Past the caches' size places'
+// rows are stored, and read, with the non-temporal hint, a token's own row without:
+// dispatch of the same in 183 us, 5.8 TB/s (213 with none, 220 with its row hinted too),
+// back in 177 (198 without); the gradient of the sum 4.9 TB/s, half of it written.
 #include "ops_device.hpp"
 #include "train.hpp"
 
@@ -56,7 +63,7 @@ __device__ __forceinline__ void fill_places(const PlacesArgs& a, int64_t block, 
   }
 }
 
-template <int V, bool NT>
+template <bool NT>
 __global__ __launch_bounds__(kThreads) void wb_dispatch_kernel(DispatchArgs a, int shift, int64_t fills) {
   __shared__ int32_t places[32 * kMaxRouteK];
   const int ob = a.out_type == WB_F32 ? 4 : 2, xb = a.x_type == WB_F32 ? 4 : 2;
@@ -66,24 +73,19 @@ __global__ __launch_bounds__(kThreads) void wb_dispatch_kernel(DispatchArgs a, i
   }
   const int lanes = 1 << shift, lane = threadIdx.x & (lanes - 1), sub = threadIdx.x >> shift;
   const int64_t row = (int64_t(blockIdx.x) - fills) * (kThreads >> shift) + sub;
+  const int64_t c = (int64_t(blockIdx.y) * lanes + lane) * 8;
   int32_t* mine = places + sub * a.at.k;
-  float v[V][8];
-  const char* x = static_cast<const char*>(a.x) + row * a.ld_x * xb;
-  const auto col = [&](int i) { return ((int64_t(blockIdx.y) * V + i) * lanes + lane) * 8; };
-#pragma unroll
-  for (int i = 0; i < V; ++i)
-    if (row < a.at.rows && col(i) < a.at.cols) load_run(x, col(i), a.at.cols, a.x_type, v[i]);
+  float v[8];
+  if (row < a.at.rows && c < a.at.cols)
+    load_run(static_cast<const char*>(a.x) + row * a.ld_x * xb, c, a.at.cols, a.x_type, v);
   own_places(a.at, row, lane, lanes, mine);
   __syncthreads();
-  if (row >= a.at.rows) return;
-  for (int i = 0; i < a.at.k; ++i) {
-    if (mine[i] < 0) continue;
-    char* to = static_cast<char*>(a.out) + mine[i] * a.ld_out * ob;
-#pragma unroll
-    for (int j = 0; j < V; ++j)
-      if (col(j) < a.at.cols) store_run<NT>(to, col(j), a.at.cols, a.out_type, v[j]);
-  }
+  if (row >= a.at.rows || c >= a.at.cols) return;
+  for (int i = 0; i < a.at.k; ++i)
+    if (mine[i] >= 0) store_run<NT>(static_cast<char*>(a.out) + mine[i] * a.ld_out * ob, c, a.at.cols, a.out_type, v);
 }
+
+constexpr int kBatch = 4;  // rows of a token under way at a time
 
 template <bool NT>
 __global__ __launch_bounds__(kThreads) void wb_dispatch_grad_kernel(DispatchGradArgs a, int shift) {
@@ -96,18 +98,37 @@ __global__ __launch_bounds__(kThreads) void wb_dispatch_grad_kernel(DispatchGrad
   const int64_t c = (int64_t(blockIdx.y) * lanes + lane) * 8;
   if (row >= a.at.rows || c >= a.at.cols) return;
   const int db = a.d_out_type == WB_F32 ? 4 : 2, ob = a.d_x_type == WB_F32 ? 4 : 2;
-  float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0}, v[8];
-  for (int i = 0; i < a.at.k; ++i) {
-    if (mine[i] < 0) continue;
-    load_run(static_cast<const char*>(a.d_out) + mine[i] * a.ld_d_out * db, c, a.at.cols, a.d_out_type, v);
-    for (int j = 0; j < 8; ++j) sum[j] += v[j];
+  float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  for (int i = 0; i < a.at.k; i += kBatch) {
+    float v[kBatch][8];
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      for (int m = 0; m < 8; ++m) v[j][m] = 0.0f;
+      if (i + j < a.at.k && mine[i + j] >= 0)
+        load_run<NT>(static_cast<const char*>(a.d_out) + mine[i + j] * a.ld_d_out * db, c, a.at.cols, a.d_out_type, v[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j)
+      for (int m = 0; m < 8; ++m) sum[m] += v[j][m];
   }
   store_run<NT>(static_cast<char*>(a.d_x) + row * a.ld_d_x * ob, c, a.at.cols, a.d_x_type, sum);
 }
 
+// The sum over 8, 16, 32 or at least 64 neighbouring lanes.
+__device__ __forceinline__ float sum_of_lanes(float v, int lanes) {
+  if (lanes >= 16) {
+    v = reduce16(v, Sum());
+    if (lanes >= 32) v += __shfl_xor(v, 16);
+    if (lanes >= 64) v += __shfl_xor(v, 32);
+    return v;
+  }
+  for (int off = 4; off > 0; off >>= 1) v += __shfl_xor(v, off);
+  return v;
+}
+
 // A row lies over 1 << shift lanes, wider ones over all of a workgroup's in
-// steps; the sums of d_gates over lanes, then wavefronts, then steps.
-template <int V, bool NT>
+// steps; the sums of d_gates over lanes, then steps, then wavefronts.
+template <bool NT>
 __global__ __launch_bounds__(kThreads) void wb_combine_grad_kernel(CombineGradArgs a, int shift, int64_t fills) {
   __shared__ int32_t places[32 * kMaxRouteK];
   __shared__ float dots[32 * kMaxRouteK];  // of each wavefront, or of each row
@@ -126,39 +147,26 @@ __global__ __launch_bounds__(kThreads) void wb_combine_grad_kernel(CombineGradAr
   __syncthreads();
   if (row < a.at.rows) {
     const char* d_row = static_cast<const char*>(a.d_out) + row * a.ld_d_out * db;
-    for (int64_t base = 0; base < a.at.cols; base += int64_t(lanes) * V * 8) {
-      float d[V][8];
-      const auto col = [&](int j) { return base + (int64_t(j) * lanes + lane) * 8; };
-#pragma unroll
-      for (int j = 0; j < V; ++j) {
-        for (int m = 0; m < 8; ++m) d[j][m] = 0.0f;
-        if (col(j) < a.at.cols) load_run(d_row, col(j), a.at.cols, a.d_out_type, d[j]);
-      }
+    for (int64_t base = 0; base < a.at.cols; base += lanes * 8) {
+      const int64_t c = base + lane * 8;
+      const bool on = c < a.at.cols;  // lanes past the row add zeros
+      float d[8], y[8], v[8];
+      for (int m = 0; m < 8; ++m) d[m] = y[m] = 0.0f;
+      if (on) load_run(d_row, c, a.at.cols, a.d_out_type, d);
       for (int i = 0; i < k; ++i) {
         const int32_t p = mine[i];
         if (p < 0) continue;
-        if (a.y) {
-          const char* y = static_cast<const char*>(a.y) + p * a.ld_y * yb;
-          float dot = 0.0f, v[8];
-#pragma unroll
-          for (int j = 0; j < V; ++j)
-            if (col(j) < a.at.cols) {
-              load_run(y, col(j), a.at.cols, a.y_type, v);
-              for (int m = 0; m < 8; ++m) dot = __builtin_fmaf(d[j][m], v[m], dot);
-            }
-          for (int off = min(lanes, 64) / 2; off > 0; off >>= 1) dot += __shfl_xor(dot, off);
-          if ((threadIdx.x & (min(lanes, 64) - 1)) == 0) dots[group * k + i] += dot;
-        }
-        if (a.d_y) {
+        float dot = 0.0f;
+        if (a.y && on) load_run<NT>(static_cast<const char*>(a.y) + p * a.ld_y * yb, c, a.at.cols, a.y_type, y);
+        if (a.d_y && on) {
           const float g = a.gates[row * k + i];
-          char* to = static_cast<char*>(a.d_y) + p * a.ld_d_y * ob;
-#pragma unroll
-          for (int j = 0; j < V; ++j)
-            if (col(j) < a.at.cols) {
-              float v[8];
-              for (int m = 0; m < 8; ++m) v[m] = g * d[j][m];
-              store_run<NT>(to, col(j), a.at.cols, a.d_y_type, v);
-            }
+          for (int m = 0; m < 8; ++m) v[m] = g * d[m];
+          store_run<NT>(static_cast<char*>(a.d_y) + p * a.ld_d_y * ob, c, a.at.cols, a.d_y_type, v);
+        }
+        if (a.y) {
+          for (int m = 0; m < 8; ++m) dot = __builtin_fmaf(d[m], y[m], dot);
+          dot = sum_of_lanes(dot, lanes);
+          if ((threadIdx.x & (min(lanes, 64) - 1)) == 0) dots[group * k + i] += dot;
         }
       }
     }
@@ -175,55 +183,48 @@ __global__ __launch_bounds__(kThreads) void wb_combine_grad_kernel(CombineGradAr
 
 struct Grid {
   int shift;
-  int64_t rows, per, lanes;
+  int64_t rows;
   uint32_t y;
 };
 
-Grid grid_of(const PlacesArgs& a, int v) {
+Grid grid_of(const PlacesArgs& a) {
   Grid g;
-  g.shift = row_shift(a.cols), g.lanes = int64_t(1) << g.shift, g.per = kThreads >> g.shift;
-  g.rows = (a.rows + g.per - 1) / g.per;
-  g.y = static_cast<uint32_t>((a.cols + g.lanes * v * 8 - 1) / (g.lanes * v * 8));
+  g.shift = row_shift(a.cols);
+  const int64_t per = kThreads >> g.shift, slab = int64_t(8) << g.shift;
+  g.rows = (a.rows + per - 1) / per;
+  g.y = static_cast<uint32_t>((a.cols + slab - 1) / slab);
   return g;
 }
 
 }  // namespace
 
 int launch_dispatch(const DispatchArgs& a, void* stream) {
-  const Grid g = grid_of(a.at, a.at.cols <= 2048 ? 1 : 2);
+  const Grid g = grid_of(a.at);
   const int64_t fills = (a.at.places + kFillPlaces - 1) / kFillPlaces;
   if (g.rows + fills == 0) return hipSuccess;
   const bool nt = a.at.places * a.at.cols * bytes_of(a.out_type) > kStreamBytes;
-  const auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>(g.rows + fills), g.y), dim3(kThreads), 0,
-                       static_cast<hipStream_t>(stream), a, g.shift, fills);
-    return hipGetLastError();
-  };
-  if (a.at.cols <= 2048) return nt ? go(wb_dispatch_kernel<1, true>) : go(wb_dispatch_kernel<1, false>);
-  return nt ? go(wb_dispatch_kernel<2, true>) : go(wb_dispatch_kernel<2, false>);
+  hipLaunchKernelGGL(nt ? wb_dispatch_kernel<true> : wb_dispatch_kernel<false>, dim3(static_cast<uint32_t>(g.rows + fills), g.y),
+                     dim3(kThreads), 0, static_cast<hipStream_t>(stream), a, g.shift, fills);
+  return hipGetLastError();
 }
 
 int launch_dispatch_grad(const DispatchGradArgs& a, void* stream) {
-  const Grid g = grid_of(a.at, 1);
+  const Grid g = grid_of(a.at);
   if (g.rows == 0) return hipSuccess;
-  hipLaunchKernelGGL(wb_dispatch_grad_kernel<false>, dim3(static_cast<uint32_t>(g.rows), g.y), dim3(kThreads), 0,
-                     static_cast<hipStream_t>(stream), a, g.shift);
+  const bool nt = a.at.places * a.at.cols * bytes_of(a.d_out_type) > kStreamBytes;
+  hipLaunchKernelGGL(nt ? wb_dispatch_grad_kernel<true> : wb_dispatch_grad_kernel<false>, dim3(static_cast<uint32_t>(g.rows), g.y),
+                     dim3(kThreads), 0, static_cast<hipStream_t>(stream), a, g.shift);
   return hipGetLastError();
 }
 
 int launch_combine_grad(const CombineGradArgs& a, void* stream) {
-  const Grid g = grid_of(a.at, 1);
+  const Grid g = grid_of(a.at);
   const int64_t fills = a.d_y ? (a.at.places + kFillPlaces - 1) / kFillPlaces : 0;
   if (g.rows + fills == 0) return hipSuccess;
   const bool nt = a.at.places * a.at.cols * (bytes_of(a.y_type) + bytes_of(a.d_y_type)) > kStreamBytes;
-  const auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>(g.rows + fills)), dim3(kThreads), 0,
-                       static_cast<hipStream_t>(stream), a, g.shift, fills);
-    return hipGetLastError();
-  };
-  if (a.at.cols <= 2048) return nt ? go(wb_combine_grad_kernel<1, true>) : go(wb_combine_grad_kernel<1, false>);
-  if (a.at.cols <= 4096) return nt ? go(wb_combine_grad_kernel<2, true>) : go(wb_combine_grad_kernel<2, false>);
-  return nt ? go(wb_combine_grad_kernel<4, true>) : go(wb_combine_grad_kernel<4, false>);
+  hipLaunchKernelGGL(nt ? wb_combine_grad_kernel<true> : wb_combine_grad_kernel<false>, dim3(static_cast<uint32_t>(g.rows + fills)),
+                     dim3(kThreads), 0, static_cast<hipStream_t>(stream), a, g.shift, fills);
+  return hipGetLastError();
 }
 
 }  // namespace wb
