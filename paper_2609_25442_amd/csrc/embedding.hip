@@ -407,10 +407,10 @@ __global__ __launch_bounds__(kThreads) void wb_embed_sum_kernel(EmbedGradArgs a,
 // run goes on in.
 constexpr int kJoinColumns = 512;
 
-__global__ __launch_bounds__(kThreads) void wb_embed_join_kernel(EmbedGradArgs a, Sorted s) {
+__global__ __launch_bounds__(kThreads) void wb_embed_join_kernel(EmbedGradArgs a, Sorted s, uint32_t slabs) {
   constexpr int kWaves = kThreads / 64;
   __shared__ float meet[kWaves][kJoinColumns];
-  const int64_t chunk = blockIdx.x, begin = chunk * s.chunk, end = begin + s.chunk;
+  const int64_t chunk = blockIdx.x / slabs, slab = blockIdx.x - chunk * slabs, begin = chunk * s.chunk, end = begin + s.chunk;
   const uint32_t v = s.keys[end - 1];
   if (v >= a.rows || s.keys[end] != v) return;
   if (s.keys[begin] == v && begin > 0 && s.keys[begin - 1] == v) return;  // it began before
@@ -425,7 +425,7 @@ __global__ __launch_bounds__(kThreads) void wb_embed_join_kernel(EmbedGradArgs a
     }
   }
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int64_t c = int64_t(blockIdx.y) * kJoinColumns + lane * 8;
+  const int64_t c = slab * kJoinColumns + lane * 8;
   float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
   if (c < a.cols) {
     if (wave == 0) load_run(reinterpret_cast<const char*>(s.partial + (chunk * 2 + 1) * a.cols), c, a.cols, WB_F32, sum);
@@ -489,8 +489,9 @@ int launch_embed(const EmbedArgs& a, void* stream) {
   const int64_t per = kThreads >> shift, runs = (a.cols + 7) / 8;
   const int64_t lanes = int64_t(1) << shift;
   const auto go = [&](auto kernel, int v) {
-    hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>((a.count + per - 1) / per), static_cast<uint32_t>((runs + lanes * v - 1) / (lanes * v))),
-                       dim3(kThreads), 0, st, a, shift);
+    const int64_t x = (a.count + per - 1) / per, y = (runs + lanes * v - 1) / (lanes * v);
+    if (!one_launch(x * y)) return hipErrorInvalidConfiguration;
+    hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>(x), static_cast<uint32_t>(y)), dim3(kThreads), 0, st, a, shift);
     return hipGetLastError();
   };
   const bool nt = a.count * a.cols * (bytes_of(a.weight_type) + bytes_of(a.out_type)) > kStreamBytes;
@@ -539,13 +540,16 @@ int launch_embed_grad(const EmbedGradArgs& a, void* stream) {
   const int64_t per = kThreads >> shift, slabs = (a.cols + (int64_t(8) << shift) - 1) / (int64_t(8) << shift);
   const int64_t sums = (s.chunks + per - 1) / per * slabs, fills = (a.rows + kFillRows - 1) / kFillRows;
   if (sums + fills == 0) return hipSuccess;
+  if (!one_launch(sums + fills)) return hipErrorInvalidConfiguration;
   const bool nt = a.cols * (a.rows * bytes_of(a.d_weight_type) + a.count * bytes_of(a.d_out_type)) > kStreamBytes;
   hipLaunchKernelGGL(nt ? wb_embed_sum_kernel<true> : wb_embed_sum_kernel<false>, dim3(static_cast<uint32_t>(sums + fills)),
                      dim3(kThreads), 0, st, a, s, shift, sums, static_cast<uint32_t>(slabs));
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || s.chunks < 2) return e;
-  hipLaunchKernelGGL(wb_embed_join_kernel, dim3(static_cast<uint32_t>(s.chunks - 1), static_cast<uint32_t>((a.cols + kJoinColumns - 1) / kJoinColumns)),
-                     dim3(kThreads), 0, st, a, s);
+  const int64_t joins = (a.cols + kJoinColumns - 1) / kJoinColumns;
+  if (!one_launch((s.chunks - 1) * joins)) return hipErrorInvalidConfiguration;
+  hipLaunchKernelGGL(wb_embed_join_kernel, dim3(static_cast<uint32_t>((s.chunks - 1) * joins)), dim3(kThreads), 0, st, a, s,
+                     static_cast<uint32_t>(joins));
   return hipGetLastError();
 }
 

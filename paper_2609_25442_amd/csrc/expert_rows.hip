@@ -202,6 +202,7 @@ int launch_dispatch(const DispatchArgs& a, void* stream) {
   const Grid g = grid_of(a.at);
   const int64_t fills = (a.at.places + kFillPlaces - 1) / kFillPlaces;
   if (g.rows + fills == 0) return hipSuccess;
+  if (!one_launch((g.rows + fills) * g.y)) return hipErrorInvalidConfiguration;
   const bool nt = a.at.places * a.at.cols * bytes_of(a.out_type) > kStreamBytes;
   hipLaunchKernelGGL(nt ? wb_dispatch_kernel<true> : wb_dispatch_kernel<false>, dim3(static_cast<uint32_t>(g.rows + fills), g.y),
                      dim3(kThreads), 0, static_cast<hipStream_t>(stream), a, g.shift, fills);
@@ -211,6 +212,7 @@ int launch_dispatch(const DispatchArgs& a, void* stream) {
 int launch_dispatch_grad(const DispatchGradArgs& a, void* stream) {
   const Grid g = grid_of(a.at);
   if (g.rows == 0) return hipSuccess;
+  if (!one_launch(g.rows * g.y)) return hipErrorInvalidConfiguration;
   const bool nt = a.at.places * a.at.cols * bytes_of(a.d_out_type) > kStreamBytes;
   hipLaunchKernelGGL(nt ? wb_dispatch_grad_kernel<true> : wb_dispatch_grad_kernel<false>, dim3(static_cast<uint32_t>(g.rows), g.y),
                      dim3(kThreads), 0, static_cast<hipStream_t>(stream), a, g.shift);
@@ -221,6 +223,7 @@ int launch_combine_grad(const CombineGradArgs& a, void* stream) {
   const Grid g = grid_of(a.at);
   const int64_t fills = a.d_y ? (a.at.places + kFillPlaces - 1) / kFillPlaces : 0;
   if (g.rows + fills == 0) return hipSuccess;
+  if (!one_launch(g.rows + fills)) return hipErrorInvalidConfiguration;
   const bool nt = a.at.places * a.at.cols * (bytes_of(a.y_type) + bytes_of(a.d_y_type)) > kStreamBytes;
   hipLaunchKernelGGL(nt ? wb_combine_grad_kernel<true> : wb_combine_grad_kernel<false>, dim3(static_cast<uint32_t>(g.rows + fills)),
                      dim3(kThreads), 0, static_cast<hipStream_t>(stream), a, g.shift, fills);

@@ -154,6 +154,9 @@ inline int row_shift(int64_t cols) {
   return shift;
 }
 
+// Whether a launch takes as many workgroups of 256: it has fewer than 2^32 threads.
+inline bool one_launch(int64_t blocks) { return blocks < (int64_t(1) << 24); }
+
 // Four neighbouring columns.
 typedef u32x2 u32x2_a2 __attribute__((aligned(2)));
 

@@ -561,6 +561,63 @@ def test_only_the_sum_of_a_norm_may_go_on():
     assert wb.add_layer_norm(y, w).total is y
 
 
+def test_gradients_of_both_parts_of_a_sum_are_their_own():
+    x, r, w = (ref.randn(*s, seed=i, dtype="bf16").cuda().requires_grad_() for i, s in enumerate([(5, 64), (5, 64), (64,)]))
+    n = wb.add_layer_norm(x, w, None, r)
+    (n.out.float().sum() + 2 * n.total.float().sum()).backward()
+    want = x.grad.clone()
+    assert torch.equal(r.grad, want)
+    x.grad.zero_()
+    assert torch.equal(r.grad, want)
+    # a tensor added to itself, and a place's weight used twice
+    y = x.detach().clone().requires_grad_()
+    n = wb.add_layer_norm(y, w.detach(), w.detach(), y)
+    n.out.backward(torch.ones_like(n.out))
+    half = wb.add_layer_norm_backward(torch.ones_like(n.out), n._replace(out=None, total=n.total.detach()), w.detach())
+    assert torch.equal(y.grad, half.x + half.residual)
+
+
+def test_a_workspace_that_is_too_small_is_refused():
+    import ctypes
+
+    from test_train_cpu import F, I64, Tokens, call, m
+
+    ids, d, w = torch.zeros(4, dtype=torch.int64, device="cuda"), torch.zeros(4, 64, device="cuda"), torch.zeros(9, 64, device="cuda")
+    at = lambda t: m(*t.shape, 0, data=t.data_ptr())  # noqa: E731
+    assert call("wb_embedding_backward", Tokens(ids.data_ptr(), 8, 0, 4), at(d), F(1), I64(0), at(w), ctypes.c_void_p(d.data_ptr()),
+                ctypes.c_size_t(16), None) == wb.WB_ESIZE
+    row, inv = w[:1], torch.ones(4, device="cuda")
+    assert call("wb_add_layer_norm_backward", at(d), at(d), at(row), None, None, ctypes.c_void_p(inv.data_ptr()), at(d), None, None, None,
+                ctypes.c_void_p(d.data_ptr()), ctypes.c_size_t(16), None) == wb.WB_ESIZE
+
+
+def test_the_gradient_may_take_its_operand_s_place():
+    """In the C calls: the norm's d_x where d_out was, the activation's where x was, the sum where the residual was."""
+    import ctypes
+
+    from test_train_cpu import call, m, F
+
+    at = lambda t: m(*(t.shape if t.dim() == 2 else (1, *t.shape)), 0, data=t.data_ptr())  # noqa: E731
+    p = lambda t: ctypes.c_void_p(t.data_ptr())  # noqa: E731
+    for cols in (72, 1501, 4099, 40001):
+        x, r, d, w = (ref.randn(*s, seed=i).cuda() for i, s in enumerate([(5, cols), (5, cols), (5, cols), (cols,)]))
+        n = wb.add_layer_norm(x, w, None, r)
+        g = wb.add_layer_norm_backward(d, n, w)
+        total, out, mean, inv = r.clone(), torch.empty_like(x), torch.empty(5, device="cuda"), torch.empty(5, device="cuda")
+        assert call("wb_add_layer_norm", at(x), at(total), at(w), None, F(1e-5), at(total), at(out), p(mean), p(inv), None) == 0
+        assert torch.equal(total, n.total) and torch.equal(out, n.out)
+        size = ctypes.c_size_t(0)
+        assert call("wb_add_layer_norm_backward_workspace", ctypes.c_int64(5), ctypes.c_int64(cols), ctypes.byref(size)) == 0
+        ws, dx, dw = torch.empty(size.value, dtype=torch.uint8, device="cuda"), d.clone(), torch.empty_like(w)
+        assert call("wb_add_layer_norm_backward", at(dx), at(total), at(w), None, p(mean), p(inv), at(dx), None, at(dw), None, p(ws), size,
+                    None) == 0
+        assert torch.equal(dx, g.x) and torch.equal(dw, g.weight)
+        a = wb.activate(x, "silu")
+        want, z = wb.activate_backward(d, a), x.clone()
+        assert call("wb_activate_backward", at(d), at(z), None, 1, 0, at(z), None) == 0
+        assert torch.equal(z, want)
+
+
 def test_a_changed_input_is_noticed_before_its_gradient():
     x = ref.randn(4, 16, seed=1).cuda().requires_grad_()
     y = x * 1
