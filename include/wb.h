@@ -673,9 +673,11 @@ int wb_combine(const wb_matrix* y, const int32_t* positions, const float* gates,
 
 /* The lookup of token embeddings, the layer norm of a residual sum, rows sorted
  * by expert and back, and the activation with a checkpoint in 8 bits, each with
- * its gradient. The conventions of the operators above hold. Gradients are sums in
+ * its gradient. The conventions of the operators above hold (a call enqueues one to
+ * three kernels, the gradient of embeddings up to eight). Gradients are sums in
  * fp32 in a fixed order, rounded once to their matrix's type; the types of a
- * gradient and of what it is of may differ. */
+ * gradient and of what it is of may differ. A call whose launch would have 2^32
+ * threads or more is refused with WB_EHIP. */
 
 /* Token ids in device memory, one after the other: int32 (bytes 4) or int64 (8). At most 4194303. */
 typedef struct wb_tokens {

@@ -11,7 +11,8 @@ and 128 columns, [rows, ceil(cols / 128)]; fp8 weights with those of 128x128
 blocks, as unpacking writes them. Arguments that do not fit raise WbError.
 Only ``route`` has a gradient: the others serve a rollout rank's tensors, and
 raise WbError for one that requires a gradient while gradients are recorded (a
-differentiable ``route``'s gates go into ``combine`` detached). Tensors with
+differentiable ``route``'s gates go into ``combine`` detached, or into the
+trainer's ``collect``). Tensors with
 a forward-mode tangent are refused by all.
 """
 
