@@ -5,9 +5,10 @@
 // in 32 us, 8.4 TB/s with what the caches hold of the frequent rows. The gradient sorts the
 // tokens (stable, so that a row's sum goes by ascending t and does not depend on
 // which workgroup ran first), sums runs of equal tokens, and writes every row of dW
-// once, the ones without a token as zeros: 16384 tokens of 128256 in 260 us, of which
-// the sort takes 24, its four launches' latency, and the 1.05 GB of dW 180 (155 without
-// the non-temporal hint, which leaves more to the calls after it: a pass takes 304 us so, 295 with it).
+// once, the ones without a token as zeros: 16384 tokens of 128256 in 250 us, of which
+// the sort takes 25, its four launches' latency, and what sums and writes the 1.05 GB of dW
+// 217 (the zeros alone 155 without the non-temporal hint, 180 with it; but a pass took 304 us
+// without, for what it left to the calls after it, and 295 with it).
 #include <algorithm>
 
 #include "ops_device.hpp"
@@ -289,7 +290,7 @@ __global__ __launch_bounds__(kSortThreads) void wb_sort_place_kernel(EmbedGradAr
 // summed and written; one that goes over an end leaves an fp32 row per chunk (0:
 // the run that came in, 1: the one that goes on), which the second launch adds.
 
-constexpr int kFillRows = 32;
+constexpr int kFillRows = 32;  // at most, to a workgroup
 constexpr int kBatch = 8;  // rows under way at a time
 
 struct Sorted {
@@ -298,6 +299,7 @@ struct Sorted {
   float* partial;  // [chunks][2][cols]
   int64_t chunks;
   int32_t chunk;  // tokens of one
+  int32_t fill;   // rows of the table to a workgroup that looks for those without a token
 };
 
 __device__ __forceinline__ void store_scaled(const EmbedGradArgs& a, uint32_t v, int64_t c, float (&sum)[8]) {
@@ -329,10 +331,10 @@ __device__ __forceinline__ void fill_rows(const EmbedGradArgs& a, const Sorted& 
   __syncthreads();
   const int64_t at = first_not_below(s.keys, a.count, v0) + threadIdx.x;
   const uint32_t key = at < a.count ? s.keys[at] : ~0u;
-  const bool mine = key < v0 + kFillRows;
+  const bool mine = key < v0 + s.fill;
   if (mine) named[key - v0] = 1;
   if (__syncthreads_and(mine)) {  // their tokens go on past the workgroup's threads
-    for (int r = threadIdx.x >> 6; r < kFillRows; r += kThreads / 64) {
+    for (int r = threadIdx.x >> 6; r < s.fill; r += kThreads / 64) {
       const int64_t first = first_not_below(s.keys, a.count, v0 + r);
       if ((threadIdx.x & 63) == 0) named[r] = first < a.count && s.keys[first] == v0 + r;
     }
@@ -340,7 +342,7 @@ __device__ __forceinline__ void fill_rows(const EmbedGradArgs& a, const Sorted& 
   }
   const int lanes = 1 << shift, lane = threadIdx.x & (lanes - 1);
   const float none[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-  for (int r = threadIdx.x >> shift; r < kFillRows; r += kThreads >> shift) {
+  for (int r = threadIdx.x >> shift; r < s.fill; r += kThreads >> shift) {
     const int64_t v = v0 + r;
     if (v >= a.rows || named[r]) continue;
     char* to = static_cast<char*>(a.d_weight) + v * a.ld_d_weight * bytes_of(a.d_weight_type);
@@ -351,7 +353,7 @@ __device__ __forceinline__ void fill_rows(const EmbedGradArgs& a, const Sorted& 
 template <bool NT>
 __global__ __launch_bounds__(kThreads) void wb_embed_sum_kernel(EmbedGradArgs a, Sorted s, int shift, int64_t sums, uint32_t slabs) {
   if (int64_t(blockIdx.x) >= sums) {
-    fill_rows<NT>(a, s, (int64_t(blockIdx.x) - sums) * kFillRows, shift);
+    fill_rows<NT>(a, s, (int64_t(blockIdx.x) - sums) * s.fill, shift);
     return;
   }
   const int lanes = 1 << shift, lane = threadIdx.x & (lanes - 1);
@@ -538,7 +540,10 @@ int launch_embed_grad(const EmbedGradArgs& a, void* stream) {
   s.chunks = (a.count + s.chunk - 1) / s.chunk;
   const int shift = row_shift(a.cols);
   const int64_t per = kThreads >> shift, slabs = (a.cols + (int64_t(8) << shift) - 1) / (int64_t(8) << shift);
-  const int64_t sums = (s.chunks + per - 1) / per * slabs, fills = (a.rows + kFillRows - 1) / kFillRows;
+  // four rows, or as many as lie side by side: many workgroups, since each begins with a search (a pass of 512 tokens, 32000 x
+  // 4096 bf16: 66 us against 69 with eight rows and 72 with 32; 16384 of 128256: 277 against 290 and 285)
+  s.fill = static_cast<int32_t>(std::max<int64_t>(4, per));
+  const int64_t sums = (s.chunks + per - 1) / per * slabs, fills = (a.rows + s.fill - 1) / s.fill;
   if (sums + fills == 0) return hipSuccess;
   if (!one_launch(sums + fills)) return hipErrorInvalidConfiguration;
   const bool nt = a.cols * (a.rows * bytes_of(a.d_weight_type) + a.count * bytes_of(a.d_out_type)) > kStreamBytes;
