@@ -169,6 +169,8 @@ def _graph():
     class Activate(Function):
         @staticmethod
         def forward(ctx, x, activation, gated, checkpoint, out_dtype):
+            # else torch makes zeros of the codes' and the scales' shapes, as gradients that nothing reads
+            ctx.set_materialize_grads(False)
             out, codes, scales = _activate(x.detach(), activation, gated, checkpoint, out_dtype)
             ctx.save_for_backward(codes if checkpoint else x, scales)
             ctx.more = activation, gated, x.dtype
@@ -179,6 +181,8 @@ def _graph():
 
         @staticmethod
         def backward(ctx, d_out, *_):
+            if d_out is None:
+                return (None,) * 5
             saved, scales = ctx.saved_tensors
             with torch.no_grad():
                 d = _activate_backward(_rows(d_out.detach()), saved.detach(), scales, *ctx.more)
