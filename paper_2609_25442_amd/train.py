@@ -149,21 +149,25 @@ def _graph():
     class Collect(Function):
         @staticmethod
         def forward(ctx, y, gates, residual, positions, tokens, span, out_dtype):
-            ctx.save_for_backward(y, gates, positions, tokens, span)
-            ctx.type = None if residual is None else residual.dtype
+            need_y, need_gates = ctx.needs_input_grad[:2]
+            # y is read for the gates' gradient alone, and none of them for the residual's
+            kept = (y if need_gates else None, gates, positions, tokens, span) if need_y or need_gates else ()
+            ctx.save_for_backward(*kept)
+            ctx.types = y.dtype, None if residual is None else residual.dtype
             return combine(plain(y), positions, plain(gates), plain(residual), span, out_dtype)
 
         @staticmethod
         def backward(ctx, d_out):
-            y, gates, positions, tokens, span = ctx.saved_tensors
             need_y, need_gates = ctx.needs_input_grad[:2]
+            of_y, of_residual = ctx.types
             d_y = d_gates = None
-            with torch.no_grad():
-                if need_y or need_gates:
-                    d_y, d_gates = _collect_backward(_rows(d_out.detach()), y.detach() if need_gates else None, positions,
-                                                     tokens, gates.detach(), span, y.dtype if need_y else None)
-            d_y, d_gates = last((d_y, d_gates), d_out, y, gates)
-            d_residual = d_out.to(ctx.type) if ctx.needs_input_grad[2] else None
+            if need_y or need_gates:
+                y, gates, positions, tokens, span = ctx.saved_tensors
+                with torch.no_grad():
+                    d_y, d_gates = _collect_backward(_rows(d_out.detach()), plain(y) if need_gates else None, positions, tokens,
+                                                     gates.detach(), span, of_y if need_y else None)
+                d_y, d_gates = last((d_y, d_gates), d_out, y, gates)
+            d_residual = d_out.to(of_residual) if ctx.needs_input_grad[2] else None
             return d_y, d_gates, d_residual, None, None, None, None
 
     class Activate(Function):
