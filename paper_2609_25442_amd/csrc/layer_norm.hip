@@ -236,6 +236,17 @@ __device__ __forceinline__ float raw_get(const Raw<TYPE>& r, int i) {
     return r.v[i >> 2][i & 3];
 }
 
+// Zeros in place of the first `n` values.
+template <int TYPE>
+__device__ __forceinline__ void raw_clear(Raw<TYPE>& r, int n) {
+  if constexpr (TYPE == WB_BF16) {
+    for (int j = 0; j < 4; ++j) r.v[j] &= n > 2 * j + 1 ? 0u : n > 2 * j ? 0xffff0000u : ~0u;
+  } else {
+    for (int i = 0; i < 8; ++i)
+      if (i < n) r.v[i >> 2][i & 3] = 0.0f;
+  }
+}
+
 template <int TT, int DT, int W, int V, bool NT>
 __global__ __launch_bounds__(64 * kGradWaves) void wb_layer_norm_grad_kernel(LayerNormGradArgs a, float* parts) {
   constexpr int G = kGradWaves / W;
@@ -246,15 +257,17 @@ __global__ __launch_bounds__(64 * kGradWaves) void wb_layer_norm_grad_kernel(Lay
   const int tb = TT == WB_F32 ? 4 : 2, db = DT == WB_F32 ? 4 : 2;
   const uint32_t cols = static_cast<uint32_t>(a.cols);
   // A lane past the row's last whole run has the row's last eight columns: those before its own, `skip` of them, are
-  // another lane's and have a weight of zero here, so that they count once.
+  // another lane's. Their gradient and their weight are zero here, so that they count once, infinite or not.
   uint32_t at_col[V];
   int skip[V];
+  bool partial = false;  // of the wavefront: whether a lane skips any
   float w[V][8], dw[V][8], sb[V][8];
 #pragma unroll
   for (int v = 0; v < V; ++v) {
     const uint32_t c = (v * (W * 64) + lane) * 8;
     at_col[v] = min(c, cols - 8);
     skip[v] = static_cast<int>(min(c - at_col[v], 8u));
+    partial = partial || __any(skip[v] > 0);
     load_eight(a.weight, at_col[v], a.weight_type, w[v]);
     for (int i = 0; i < 8; ++i) {
       if (i < skip[v]) w[v][i] = 0.0f;
@@ -294,6 +307,10 @@ __global__ __launch_bounds__(64 * kGradWaves) void wb_layer_norm_grad_kernel(Lay
 #pragma unroll
     for (int v = 0; v < V; ++v) tc[v] = t[v], mc[v] = more[v], dc[v] = d[v];
     fetch(row + step);
+    if (partial) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) raw_clear(dc[v], skip[v]);
+    }
     float s1 = 0.0f, s2 = 0.0f;
     if (row < a.rows) {
 #pragma unroll
