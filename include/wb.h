@@ -730,12 +730,12 @@ int wb_add_layer_norm_backward(const wb_matrix* d_out, const wb_matrix* total, c
                                void* workspace, size_t workspace_bytes, void* stream);
 
 /* Rows by expert: out[positions[t, i]] = x[t] for T rows of k choices, zeros in
- * the other rows of out [places, cols] (those past the last place). positions [T, k] and
- * tokens [places] are wb_routing's: positions[t, i] is a place of which tokens says t,
- * and no place is named twice; what is not so, is outside 0..places-1, or
- * outside first[0] <= place < last[0] where these device pointers are given, is
- * left out. 1 <= k <= 64, places < 2^31. x and out are WB_F32 or WB_BF16.
- * Errors: WB_EINVAL, WB_EUNSUPPORTED, WB_EHIP. */
+ * the other rows of out [places, cols]. positions [T, k] and tokens [places] are
+ * wb_routing's. A choice counts if its place is one of 0..places-1 (and first[0] <=
+ * place < last[0] where these device pointers are given), tokens says t there, and
+ * no earlier choice of t has the same place; any other integers are left out, here
+ * and in the gradients below. 1 <= k <= 64, places < 2^31. x and out are WB_F32 or
+ * WB_BF16. Errors: WB_EINVAL, WB_EUNSUPPORTED, WB_EHIP. */
 int wb_dispatch(const wb_matrix* x, const int32_t* positions, const int32_t* tokens, int32_t k, const int32_t* first,
                 const int32_t* last, const wb_matrix* out, void* stream);
 /* d_x[t] = sum over i of d_out[positions[t, i]], in the order of i; the same places are left out. */

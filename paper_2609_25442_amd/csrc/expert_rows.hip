@@ -3,8 +3,8 @@
 //   combine's gradient: dy_p = g_ti dout_t, zeros elsewhere;  dg_ti = <dout_t, y_p>
 // (the sum itself is in route.hip). Work goes by tokens: a token's row is read
 // once and its k places are written, or read, from there. A place is a token's
-// own if tokens says so, so no two rows write one place; the places that are
-// nobody's are filled with zeros by workgroups of their own.
+// own if tokens says so, so no two rows write one place, and counts once in a
+// row; the places that are nobody's are filled with zeros by workgroups of their own.
 //
 // Bandwidth bound: eight columns a thread, one run of them, since what hides a
 // row's way to memory here is the number of wavefronts (the gradient of 8192 x
@@ -26,16 +26,30 @@ __device__ __forceinline__ int64_t last_place(const PlacesArgs& a) {
   return a.last ? min(a.places, int64_t(*a.last)) : a.places;
 }
 
-// A row's own places into LDS, -1 for what is left out.
+// A row's own places into LDS, -1 for what is left out: a place outside the
+// call's, one that tokens gives to another row, and, with ONCE, one that an earlier
+// choice of the row has. A row's choices are those of one wavefront's lanes.
+template <bool ONCE>
 __device__ __forceinline__ void own_places(const PlacesArgs& a, int64_t row, int lane, int lanes, int32_t* to) {
   const int64_t first = first_place(a), last = last_place(a);
   for (int i = lane; i < a.k; i += lanes) {
-    int32_t p = -1;
-    if (row < a.rows) {
-      p = a.positions[row * a.k + i];
-      if (p < first || p >= last || a.tokens[p] != row) p = -1;
+    const int32_t p = row < a.rows ? a.positions[row * a.k + i] : -1;
+    const int32_t of = p >= first && p < last ? a.tokens[p] : -1;
+    bool again = false;
+    if (ONCE) {
+      to[i] = p;
+      order_lanes();
+      // what is -1 here already was left out itself, and so is the same place after it
+      for (int j = 0; j < i; j += 8) {
+        int32_t before[8];
+#pragma unroll
+        for (int m = 0; m < 8; ++m) before[m] = to[min(j + m, i - 1)];
+#pragma unroll
+        for (int m = 0; m < 8; ++m) again = again || before[m] == p;
+      }
+      order_lanes();
     }
-    to[i] = p;
+    to[i] = of == row && !again ? p : -1;
   }
 }
 
@@ -78,7 +92,7 @@ __global__ __launch_bounds__(kThreads) void wb_dispatch_kernel(DispatchArgs a, i
   float v[8];
   if (row < a.at.rows && c < a.at.cols)
     load_run(static_cast<const char*>(a.x) + row * a.ld_x * xb, c, a.at.cols, a.x_type, v);
-  own_places(a.at, row, lane, lanes, mine);
+  own_places<false>(a.at, row, lane, lanes, mine);  // written twice, a place holds the same
   __syncthreads();
   if (row >= a.at.rows || c >= a.at.cols) return;
   for (int i = 0; i < a.at.k; ++i)
@@ -93,7 +107,7 @@ __global__ __launch_bounds__(kThreads) void wb_dispatch_grad_kernel(DispatchGrad
   const int lanes = 1 << shift, lane = threadIdx.x & (lanes - 1), sub = threadIdx.x >> shift;
   const int64_t row = int64_t(blockIdx.x) * (kThreads >> shift) + sub;
   int32_t* mine = places + sub * a.at.k;
-  own_places(a.at, row, lane, lanes, mine);
+  own_places<true>(a.at, row, lane, lanes, mine);
   __syncthreads();
   const int64_t c = (int64_t(blockIdx.y) * lanes + lane) * 8;
   if (row >= a.at.rows || c >= a.at.cols) return;
@@ -142,7 +156,7 @@ __global__ __launch_bounds__(kThreads) void wb_combine_grad_kernel(CombineGradAr
   const int64_t row = (int64_t(blockIdx.x) - fills) * (kThreads >> shift) + sub;
   const int group = lanes < 64 ? sub : int(threadIdx.x >> 6), groups = lanes < 64 ? 1 : lanes >> 6;
   int32_t* mine = places + sub * k;
-  own_places(a.at, row, lane, lanes, mine);
+  own_places<true>(a.at, row, lane, lanes, mine);
   for (int i = threadIdx.x; i < (kThreads / min(lanes, 64)) * k; i += kThreads) dots[i] = 0.0f;
   __syncthreads();
   if (row < a.at.rows) {
