@@ -741,11 +741,18 @@ int wb_dispatch(const wb_matrix* x, const int32_t* positions, const int32_t* tok
 /* d_x[t] = sum over i of d_out[positions[t, i]], in the order of i; the same places are left out. */
 int wb_dispatch_backward(const wb_matrix* d_out, const int32_t* positions, const int32_t* tokens, int32_t k,
                          const int32_t* first, const int32_t* last, const wb_matrix* d_x, void* stream);
-/* Gradients of wb_combine over wb_routing's places:
+/* out[t] = residual[t] + sum_i gates[t, i] * y[positions[t, i]] over the choices
+ * that count as in wb_dispatch, summed in fp32 in the order of i: over wb_routing's
+ * places what wb_combine computes, bit for bit. gates are WB_F32 [T, k]; residual may
+ * be NULL. y, residual and out are WB_F32 or WB_BF16; out may be the residual itself,
+ * where the types are alike. Errors as wb_dispatch. */
+int wb_collect(const wb_matrix* y, const int32_t* positions, const int32_t* tokens, const float* gates, int32_t k,
+               const wb_matrix* residual, const int32_t* first, const int32_t* last, const wb_matrix* out, void* stream);
+/* Its gradients:
  *   d_y[positions[t, i]] = gates[t, i] * d_out[t], zeros in y's other rows
- *   d_gates[t, i] = sum over columns of d_out[t] * y[positions[t, i]], 0 where the place is left out
- * (the residual's is d_out). Places as in wb_dispatch. y and d_gates may both be NULL, or
- * d_y; y has d_y's shape. Errors as wb_dispatch. */
+ *   d_gates[t, i] = sum over columns of d_out[t] * y[positions[t, i]], 0 where the choice is left out
+ * (the residual's is d_out). y and d_gates may both be NULL, or d_y; y has d_y's
+ * shape. Errors as wb_dispatch. */
 int wb_combine_backward(const wb_matrix* d_out, const wb_matrix* y, const int32_t* positions, const int32_t* tokens,
                         const float* gates, int32_t k, const int32_t* first, const int32_t* last, const wb_matrix* d_y,
                         float* d_gates, void* stream);

@@ -94,6 +94,7 @@ PyMethodDef methods[] = {
     {"add_layer_norm_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(wb_py_add_layer_norm_backward)), METH_FASTCALL, nullptr},
     {"dispatch", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(wb_py_dispatch)), METH_FASTCALL, nullptr},
     {"dispatch_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(wb_py_dispatch_backward)), METH_FASTCALL, nullptr},
+    {"collect", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(wb_py_collect)), METH_FASTCALL, nullptr},
     {"collect_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(wb_py_collect_backward)), METH_FASTCALL, nullptr},
     {"activate", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(wb_py_activate)), METH_FASTCALL, nullptr},
     {"activate_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(wb_py_activate_backward)), METH_FASTCALL, nullptr},

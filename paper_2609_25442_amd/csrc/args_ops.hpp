@@ -16,6 +16,7 @@ PyObject* wb_py_add_layer_norm(PyObject*, PyObject* const* args, Py_ssize_t n);
 PyObject* wb_py_add_layer_norm_backward(PyObject*, PyObject* const* args, Py_ssize_t n);
 PyObject* wb_py_dispatch(PyObject*, PyObject* const* args, Py_ssize_t n);
 PyObject* wb_py_dispatch_backward(PyObject*, PyObject* const* args, Py_ssize_t n);
+PyObject* wb_py_collect(PyObject*, PyObject* const* args, Py_ssize_t n);
 PyObject* wb_py_collect_backward(PyObject*, PyObject* const* args, Py_ssize_t n);
 PyObject* wb_py_activate(PyObject*, PyObject* const* args, Py_ssize_t n);
 PyObject* wb_py_activate_backward(PyObject*, PyObject* const* args, Py_ssize_t n);

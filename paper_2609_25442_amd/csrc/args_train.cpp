@@ -230,6 +230,33 @@ PyObject* wb_py_dispatch_backward(PyObject*, PyObject* const* args, Py_ssize_t n
   });
 }
 
+// collect(fn, y, positions, tokens, gates, residual, span, out_dtype, device, stream) -> out
+PyObject* wb_py_collect(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (!counted(n, 10, "collect")) return nullptr;
+  return guarded([&]() -> PyObject* {
+    const Where at(args + 8);
+    const long type = PyLong_AsLong(args[7]);
+    auto* fn = function<decltype(wb_collect)>(args[0]);
+    if (PyErr_Occurred()) return nullptr;
+    const Tensor& y = needed(args[1], "y", at.device);
+    const Places p(needed(args[2], "positions", at.device), needed(args[3], "tokens", at.device));
+    const Tensor& gates = needed(args[4], "gates", at.device);
+    const Tensor* residual = tensor(args[5], "residual", at.device);
+    const Span span(tensor(args[6], "span", at.device));
+    ungraded({{&y, "y"}, {&gates, "gates"}, {residual, "residual"}});
+    plain(gates, at::kFloat, p.rows * p.k, "gates");
+    const wb_matrix my = matrix(y, "y");
+    if (my.rows != p.places) refuse("y", "has another number of rows than the routing has places");
+    wb_matrix mr{};
+    if (residual) mr = matrix(*residual, "residual");
+    Tensor out = fresh({p.rows, my.cols}, type_of(type < 0 ? my.dtype : static_cast<int32_t>(type)), y);
+    const wb_matrix mo = matrix(out, "out");
+    const int rc = fn(&my, p.positions, p.tokens, gates.data_ptr<float>(), static_cast<int32_t>(p.k), residual ? &mr : nullptr,
+                      span.first, span.last, &mo, at.stream);
+    return rc != WB_OK ? PyLong_FromLong(rc) : wrap(out);
+  });
+}
+
 // collect_backward(fn, d_out, y, positions, tokens, gates, span, y_type, device, stream) -> (d_y, d_gates)
 // y None: no d_gates; y_type -1: no d_y
 PyObject* wb_py_collect_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {

@@ -90,6 +90,16 @@ struct DispatchGradArgs {
   int32_t d_out_type, d_x_type;
 };
 
+struct CollectArgs {
+  PlacesArgs at;
+  const void* y;
+  const float* gates;
+  const void* residual;  // null: none
+  void* out;
+  int64_t ld_y, ld_residual, ld_out;
+  int32_t y_type, residual_type, out_type;
+};
+
 struct CombineGradArgs {
   PlacesArgs at;
   const void* d_out;
@@ -133,6 +143,7 @@ int launch_layer_norm(const LayerNormArgs& a, void* stream);
 int launch_layer_norm_grad(const LayerNormGradArgs& a, void* stream);
 int launch_dispatch(const DispatchArgs& a, void* stream);
 int launch_dispatch_grad(const DispatchGradArgs& a, void* stream);
+int launch_collect(const CollectArgs& a, void* stream);
 int launch_combine_grad(const CombineGradArgs& a, void* stream);
 int launch_activate(const ActivateArgs& a, void* stream);
 int launch_activate_grad(const ActivateGradArgs& a, void* stream);

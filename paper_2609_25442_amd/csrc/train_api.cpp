@@ -252,6 +252,28 @@ int wb_dispatch_backward(const wb_matrix* d_out, const int32_t* positions, const
   });
 }
 
+int wb_collect(const wb_matrix* y, const int32_t* positions, const int32_t* tokens, const float* gates, int32_t k,
+               const wb_matrix* residual, const int32_t* first, const int32_t* last, const wb_matrix* out, void* stream) {
+  return guarded([&]() -> int {
+    if (!y || !out) return set_error(WB_EINVAL, "null argument");
+    Operands ops;
+    wb::CollectArgs a{};
+    const int rc = check_places(*out, *y, positions, tokens, k, first, last, ops, a.at);
+    if (rc != WB_OK) return rc;
+    floats(ops, *y, y->rows, out->cols, "y");
+    ops.array(gates, out->rows * k, 4, "gates");
+    if (residual) {
+      floats(ops, *residual, out->rows, out->cols, "residual");
+      a.residual = residual->data, a.residual_type = residual->dtype, a.ld_residual = residual->ld;
+    }
+    floats(ops, *out, out->rows, out->cols, "out");
+    if (ops.rc != WB_OK) return ops.rc;
+    a.y = y->data, a.y_type = y->dtype, a.ld_y = y->ld, a.gates = gates;
+    a.out = out->data, a.out_type = out->dtype, a.ld_out = out->ld;
+    return launched(wb::launch_collect(a, stream), "collect launch");
+  });
+}
+
 int wb_combine_backward(const wb_matrix* d_out, const wb_matrix* y, const int32_t* positions, const int32_t* tokens,
                         const float* gates, int32_t k, const int32_t* first, const int32_t* last, const wb_matrix* d_y,
                         float* d_gates, void* stream) {

@@ -23,7 +23,7 @@ from __future__ import annotations
 import collections
 
 from . import DTYPES, WB_EINVAL, WB_EUNSUPPORTED, WbError, _args
-from .ops import ACTIVATIONS, _address, _grad_enabled, _here, _on, _refused, _type, combine
+from .ops import ACTIVATIONS, _address, _grad_enabled, _here, _on, _refused, _type
 
 
 def _result(r):
@@ -91,7 +91,7 @@ def _graph():
             raise WbError(WB_EINVAL, "an argument has a forward-mode tangent, which the operators do not carry on")
 
     def plain(t):
-        return None if t is None else t.detach()
+        return t.detach() if isinstance(t, torch.Tensor) else t
 
     class Embedding(Function):
         @staticmethod
@@ -149,12 +149,13 @@ def _graph():
     class Collect(Function):
         @staticmethod
         def forward(ctx, y, gates, residual, positions, tokens, span, out_dtype):
+            out = _collect(plain(y), positions, tokens, plain(gates), plain(residual), span, out_dtype)
             need_y, need_gates = ctx.needs_input_grad[:2]
             # y is read for the gates' gradient alone, and none of them for the residual's
             kept = (y if need_gates else None, gates, positions, tokens, span) if need_y or need_gates else ()
             ctx.save_for_backward(*kept)
             ctx.types = y.dtype, None if residual is None else residual.dtype
-            return combine(plain(y), positions, plain(gates), plain(residual), span, out_dtype)
+            return out
 
         @staticmethod
         def backward(ctx, d_out):
@@ -318,16 +319,16 @@ def dispatch_backward(d_rows, routing, span=None, out_dtype=None, stream=None):
 def collect(y, routing, gates=None, residual=None, span=None, out_dtype=None, stream=None):
     """``residual[t] + sum_i gates[t, i] * y[routing.positions[t, i]]``: what
     ``combine`` computes, differentiable in y [T * k, cols], gates (default:
-    ``routing.gates``) and residual. ``span`` and ``out_dtype`` as there."""
+    ``routing.gates``) and residual. ``span`` and ``out_dtype`` as there.
+    Choices whose place ``routing.tokens`` gives to another row, or that name a
+    place again, are left out, as they are by ``dispatch``."""
     if stream is not None:
         return _on(stream, lambda: collect(y, routing, gates, residual, span, out_dtype), y, routing.positions,
                    routing.tokens, routing.gates, gates, residual, span)
     gates = routing.gates if gates is None else gates
-    if getattr(y, "ndim", 2) == 2 and y.shape[0] != routing.tokens.shape[0]:
-        raise WbError(WB_EINVAL, "y has another number of rows than the routing has places")
     if _differentiated(y, gates, residual):
         return _graph()["collect"](y, gates, residual, routing.positions, routing.tokens, span, out_dtype)
-    return combine(y, routing.positions, gates, residual, span, out_dtype)
+    return _collect(y, routing.positions, routing.tokens, gates, residual, span, out_dtype)
 
 
 def collect_backward(d_out, y, routing, gates=None, span=None, stream=None):
@@ -347,6 +348,11 @@ def _dispatch(x, positions, tokens, span):
 
 def _dispatch_backward(d_rows, positions, tokens, span, type_):
     return _result(_args.dispatch_backward(_address("wb_dispatch_backward"), d_rows, positions, tokens, span, type_, *_here()))
+
+
+def _collect(y, positions, tokens, gates, residual, span, out_dtype):
+    return _result(_args.collect(_address("wb_collect"), y, positions, tokens, gates, residual, span,
+                                 _type(out_dtype, DTYPES, "out_dtype"), *_here()))
 
 
 def _collect_backward(d_out, y, positions, tokens, gates, span, y_type):

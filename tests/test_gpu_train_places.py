@@ -1,4 +1,4 @@
-"""dispatch and its gradient, and collect's, over integers that no router wrote:
+"""dispatch and collect, there and back, over integers that no router wrote:
 places outside the rows, of other rows, and named twice. A choice counts where
 its place is one of the call's, says its row, and no earlier choice of the row
 has it; the operators and their gradients agree on that."""
@@ -54,7 +54,7 @@ def test_operators_and_gradients_agree_on_what_counts(shape):
     for t, span in (("f32", None), ("bf16", None), ("f32", [places // 4, places - places // 3])):
         on = counts(positions, tokens, span)
         where = None if span is None else torch.tensor(span, dtype=torch.int32, device="cuda")
-        x, d = (ref.randn(rows, cols, seed=s, dtype=t) for s in (1, 2))
+        x, d, res = (ref.randn(rows, cols, seed=s, dtype=t) for s in (1, 2, 3))
         y = ref.randn(places, cols, seed=4, dtype=t)
         gates = ref.randn(rows, k, seed=5)
         r = of(positions, tokens, gates)
@@ -68,6 +68,10 @@ def test_operators_and_gradients_agree_on_what_counts(shape):
         size.index_add_(0, row, y.double()[at].abs())
         ref.check(wb.dispatch_backward(y.cuda(), r, span=where), dx, size * U32 * k, "dispatch's gradient")
         g = gates.double()[row, i][:, None]
+        out, size = res.double(), res.double().abs()
+        out.index_add_(0, row, g * y.double()[at])
+        size.index_add_(0, row, (g * y.double()[at]).abs())
+        ref.check(wb.collect(y.cuda(), r, residual=res.cuda(), span=where), out, size * U32 * (k + 1), "collect")
         d_y, d_g = wb.collect_backward(d.cuda(), y.cuda(), r, span=where)
         of_y, of_g, e_g = torch.zeros(places, cols).double(), torch.zeros(rows, k).double(), torch.zeros(rows, k).double()
         of_y[at] = g * d.double()[row]
@@ -84,5 +88,56 @@ def test_a_place_named_twice_in_a_row_is_the_first_choice_s():
     x, y = torch.ones(2, 16, device="cuda"), torch.ones(4, 16, device="cuda")
     assert wb.dispatch(x, r)[:, 0].tolist() == [1, 1, 1, 0]
     assert wb.dispatch_backward(y, r)[:, 0].tolist() == [2, 1]
+    assert wb.collect(y, r)[:, 0].tolist() == [7, 7]
     d_y, d_g = wb.collect_backward(x, y, r)
     assert d_y[:, 0].tolist() == [5, 2, 7, 0] and d_g.tolist() == [[16, 0, 16], [16, 0, 0]]
+
+
+def test_collect_of_places_that_say_another_row():
+    """An edited routing: a place that tokens no longer gives to a row adds nothing, as its gradients are zeros."""
+    z = ref.randn(12, 6, seed=1).cuda()
+    r = wb.route(z, 2)
+    gone = r.positions[3, 1].item()
+    tokens = r.tokens.clone()
+    tokens[gone] = -1
+    edited = r._replace(tokens=tokens)
+    y = ref.randn(24, 40, seed=2).cuda()
+    y[gone] = float("nan")
+    gates = r.gates.clone().requires_grad_()
+    rows = y.clone().requires_grad_()
+    out = wb.collect(rows, edited, gates=gates)
+    assert torch.isfinite(out).all()
+    out.sum().backward()
+    assert gates.grad[3, 1] == 0 and torch.isfinite(gates.grad).all() and not rows.grad[gone].any()
+    other = torch.arange(12, device="cuda") != 3
+    assert torch.equal(out[other], wb.combine(y, r.positions, r.gates)[other])
+
+
+def test_collect_refuses_what_is_no_tensor():
+    r = of(torch.zeros(2, 1).long(), torch.zeros(2).long(), torch.ones(2, 1))
+    x = torch.ones(2, 8, device="cuda")
+    for call in (lambda: wb.collect(None, r), lambda: wb.collect([1.0], r), lambda: wb.collect(x[0], r), lambda: wb.collect(x[:1], r),
+                 lambda: wb.collect(None, r, gates=torch.ones(2, 1, device="cuda", requires_grad=True)),
+                 lambda: wb.collect(x, r._replace(tokens=r.tokens.long())), lambda: wb.collect(x, r, span=r.tokens.long()),
+                 lambda: wb.collect(x, r, out_dtype="f8e4m3"), lambda: wb.collect(x.half(), r), lambda: wb.collect(x, r, residual=x[:1])):
+        with pytest.raises(wb.WbError):
+            call()
+
+
+def test_collect_into_the_residual_s_place_and_of_rows_that_start_anywhere():
+    import ctypes
+
+    from test_train_cpu import call, m
+
+    r = wb.route(ref.randn(30, 8, seed=1).cuda(), 3)
+    p = lambda v: ctypes.c_void_p(v.data_ptr())  # noqa: E731
+    for cols in (72, 1501, 4099):
+        y, res = ref.randn(90, cols, seed=2), ref.randn(30, cols, seed=3)
+        want = wb.collect(y.cuda(), r, residual=res.cuda())
+        assert torch.equal(want, wb.combine(y.cuda(), r.positions, r.gates, residual=res.cuda()))
+        for pad, skip in ((0, 1), (3, 0), (5, 3)):
+            assert torch.equal(wb.collect(ref.strided(y, pad, skip), r, residual=ref.strided(res, pad, skip)), want)
+        here, rows = res.cuda(), y.cuda()
+        at = lambda v: m(*v.shape, 0, data=v.data_ptr())  # noqa: E731
+        assert call("wb_collect", at(rows), p(r.positions), p(r.tokens), p(r.gates), 3, at(here), None, None, at(here), None) == 0
+        assert torch.equal(here, want)

@@ -64,7 +64,7 @@ def test_an_activation_whose_result_got_no_gradient_has_none(received):
                                    (True, True, True)], ids=str)
 def test_collect_keeps_expert_rows_for_the_gates_alone(monkeypatch, needs):
     """T * k rows that no gradient reads are not held: a frozen router's gates need none of them."""
-    monkeypatch.setattr(train, "combine", lambda y, *_: y[:2] * 1.0)
+    monkeypatch.setattr(train, "_collect", lambda y, *_: y[:2] * 1.0)
     calls = []
 
     def collect_backward(d_out, y, positions, tokens, gates, span, y_type):
