@@ -478,7 +478,33 @@ Layout layout_of(int64_t count, int64_t rows, int64_t cols) {
   return l;
 }
 
+// The launches after the sort: workgroups of the sums, of the rows without a
+// token, and of the joins.
+struct Grids {
+  int shift;
+  int32_t chunk, fill;
+  int64_t chunks, slabs, sums, fills, joins;  // joins: to a chunk
+  bool fit() const { return one_launch(sums + fills) && (chunks < 2 || one_launch((chunks - 1) * joins)); }
+};
+
+Grids grids_of(int64_t count, int64_t rows, int64_t cols) {
+  Grids g;
+  g.shift = row_shift(cols);
+  g.chunk = chunk_of(count);
+  g.chunks = (count + g.chunk - 1) / g.chunk;
+  const int64_t per = kThreads >> g.shift;
+  g.slabs = (cols + (int64_t(8) << g.shift) - 1) / (int64_t(8) << g.shift);
+  // four rows, or as many as lie side by side: many workgroups, since each begins with a search (a pass of 512 tokens, 32000 x
+  // 4096 bf16: 66 us against 69 with eight rows and 72 with 32; 16384 of 128256: 277 against 290 and 285)
+  g.fill = static_cast<int32_t>(std::max<int64_t>(4, per));
+  g.sums = (g.chunks + per - 1) / per * g.slabs, g.fills = (rows + g.fill - 1) / g.fill;
+  g.joins = (cols + kJoinColumns - 1) / kJoinColumns;
+  return g;
+}
+
 }  // namespace
+
+bool embed_grad_fits(int64_t count, int64_t rows, int64_t cols) { return grids_of(count, rows, cols).fit(); }
 
 size_t embed_grad_workspace_bytes(int64_t count, int64_t rows, int64_t cols) {
   return static_cast<size_t>(layout_of(count, rows, cols).all);
@@ -502,6 +528,7 @@ int launch_embed(const EmbedArgs& a, void* stream) {
 }
 
 int launch_embed_grad(const EmbedGradArgs& a, void* stream) {
+  const Grids g = grids_of(a.count, a.rows, a.cols);  // embed_grad_fits has said that they fit
   const auto st = static_cast<hipStream_t>(stream);
   char* ws = static_cast<char*>(a.workspace);
   const Layout l = layout_of(a.count, a.rows, a.cols);
@@ -536,25 +563,15 @@ int launch_embed_grad(const EmbedGradArgs& a, void* stream) {
   }
   Sorted s{};
   s.keys = keys(now), s.order = order(now), s.partial = reinterpret_cast<float*>(ws + l.partial);
-  s.chunk = chunk_of(a.count);
-  s.chunks = (a.count + s.chunk - 1) / s.chunk;
-  const int shift = row_shift(a.cols);
-  const int64_t per = kThreads >> shift, slabs = (a.cols + (int64_t(8) << shift) - 1) / (int64_t(8) << shift);
-  // four rows, or as many as lie side by side: many workgroups, since each begins with a search (a pass of 512 tokens, 32000 x
-  // 4096 bf16: 66 us against 69 with eight rows and 72 with 32; 16384 of 128256: 277 against 290 and 285)
-  s.fill = static_cast<int32_t>(std::max<int64_t>(4, per));
-  const int64_t sums = (s.chunks + per - 1) / per * slabs, fills = (a.rows + s.fill - 1) / s.fill;
-  if (sums + fills == 0) return hipSuccess;
-  if (!one_launch(sums + fills)) return hipErrorInvalidConfiguration;
+  s.chunk = g.chunk, s.chunks = g.chunks, s.fill = g.fill;
+  if (g.sums + g.fills == 0) return hipSuccess;
   const bool nt = a.cols * (a.rows * bytes_of(a.d_weight_type) + a.count * bytes_of(a.d_out_type)) > kStreamBytes;
-  hipLaunchKernelGGL(nt ? wb_embed_sum_kernel<true> : wb_embed_sum_kernel<false>, dim3(static_cast<uint32_t>(sums + fills)),
-                     dim3(kThreads), 0, st, a, s, shift, sums, static_cast<uint32_t>(slabs));
+  hipLaunchKernelGGL(nt ? wb_embed_sum_kernel<true> : wb_embed_sum_kernel<false>, dim3(static_cast<uint32_t>(g.sums + g.fills)),
+                     dim3(kThreads), 0, st, a, s, g.shift, g.sums, static_cast<uint32_t>(g.slabs));
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || s.chunks < 2) return e;
-  const int64_t joins = (a.cols + kJoinColumns - 1) / kJoinColumns;
-  if (!one_launch((s.chunks - 1) * joins)) return hipErrorInvalidConfiguration;
-  hipLaunchKernelGGL(wb_embed_join_kernel, dim3(static_cast<uint32_t>((s.chunks - 1) * joins)), dim3(kThreads), 0, st, a, s,
-                     static_cast<uint32_t>(joins));
+  if (e != hipSuccess || g.chunks < 2) return e;
+  hipLaunchKernelGGL(wb_embed_join_kernel, dim3(static_cast<uint32_t>((g.chunks - 1) * g.joins)), dim3(kThreads), 0, st, a, s,
+                     static_cast<uint32_t>(g.joins));
   return hipGetLastError();
 }
 

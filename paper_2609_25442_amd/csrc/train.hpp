@@ -133,6 +133,7 @@ struct ActivateGradArgs {
   bool gated;
 };
 
+bool embed_grad_fits(int64_t count, int64_t rows, int64_t cols);  // whether its launches take these sizes
 size_t embed_grad_workspace_bytes(int64_t count, int64_t rows, int64_t cols);
 size_t layer_norm_grad_workspace_bytes(int64_t rows, int64_t cols);
 

@@ -41,14 +41,13 @@ int check_workspace(Operands& ops, const void* workspace, size_t bytes, size_t n
 }
 
 // Token ids, and the table of `rows` that they name rows of.
-int check_tokens(const wb_tokens* t, int64_t rows, int64_t first, Operands& ops) {
+int check_tokens(const wb_tokens* t, int64_t rows, int64_t first) {
   if (t->bytes != 4 && t->bytes != 8) return set_error(WB_EINVAL, "tokens are neither int32 nor int64");
   int rc = too_many_rows(t->count);
   if (rc == WB_OK) rc = too_many_rows(rows);
   if (rc != WB_OK) return rc;
   if (first < 0 || first > kMaxFirst) return set_error(WB_EINVAL, "first is outside 0..2^62");
-  ops.array(t->data, t->count, t->bytes, "tokens");
-  return ops.rc;
+  return WB_OK;
 }
 
 int check_places(const wb_matrix& by_row, const wb_matrix& by_place, const int32_t* positions, const int32_t* tokens, int32_t k,
@@ -89,9 +88,10 @@ int wb_embedding(const wb_tokens* tokens, const wb_matrix* weight, float scale, 
   return guarded([&]() -> int {
     if (!tokens || !weight || !out) return set_error(WB_EINVAL, "null argument");
     Operands ops;
-    int rc = check_tokens(tokens, weight->rows, first, ops);
+    int rc = check_tokens(tokens, weight->rows, first);
     if (rc == WB_OK) rc = check_sizes(weight->rows, weight->cols);
     if (rc != WB_OK) return rc;
+    ops.array(tokens->data, tokens->count, tokens->bytes, "tokens");
     floats(ops, *weight, weight->rows, weight->cols, "weight");
     floats(ops, *out, tokens->count, weight->cols, "out");
     if (ops.rc != WB_OK) return ops.rc;
@@ -119,9 +119,13 @@ int wb_embedding_backward(const wb_tokens* tokens, const wb_matrix* d_out, float
   return guarded([&]() -> int {
     if (!tokens || !d_out || !d_weight) return set_error(WB_EINVAL, "null argument");
     Operands ops;
-    int rc = check_tokens(tokens, d_weight->rows, first, ops);
+    int rc = check_tokens(tokens, d_weight->rows, first);
     if (rc == WB_OK) rc = check_sizes(d_weight->rows, d_weight->cols);
     if (rc != WB_OK) return rc;
+    // ahead of its first launch: a refused call writes nothing
+    if (!wb::embed_grad_fits(tokens->count, d_weight->rows, d_weight->cols))
+      return launched(hipErrorInvalidConfiguration, "embedding gradient launch");
+    ops.array(tokens->data, tokens->count, tokens->bytes, "tokens");
     floats(ops, *d_out, tokens->count, d_weight->cols, "d_out");
     floats(ops, *d_weight, d_weight->rows, d_weight->cols, "d_weight");
     rc = check_workspace(ops, workspace, workspace_bytes,

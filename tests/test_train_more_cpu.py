@@ -28,3 +28,17 @@ def test_collect_refuses(more, code):
 def test_collect_refuses_without_arguments():
     assert call("wb_collect", None, P, P, P, 1, None, None, None, m(1, 1), None) == E
     assert call("wb_collect", m(1, 1), P, P, P, 1, None, None, None, None, None) == E
+
+
+@pytest.mark.parametrize("count,rows,cols,code", [
+    (8192, 1, 1 << 26, wb.WB_EHIP),        # the joins' launch
+    (4194303, 1, 1 << 20, wb.WB_EHIP),     # the sums' one too
+    (8192, 4194303, 1 << 22, E), (4194303, 4194303, 8192, E), (16, 9, 1 << 26, E),  # one launch takes these: refused for their memory
+])
+def test_an_embedding_gradient_past_a_launch_is_refused_before_anything_else(count, rows, cols, code):
+    """Before its memory is looked up, and so before its first launch, which would leave d_weight partly written."""
+    from test_train_cpu import F, I64, ids
+
+    assert call("wb_embedding_backward", ids(count), m(count, cols), F(1), I64(0), m(rows, cols), P, ctypes.c_size_t(1 << 50), None) == code
+    if code == wb.WB_EHIP:
+        assert b"embedding gradient" in wb.lib.wb_last_error()
