@@ -693,8 +693,12 @@ typedef struct wb_tokens {
  * most 4194303. Errors: WB_EINVAL, WB_EUNSUPPORTED, WB_EHIP. */
 int wb_embedding(const wb_tokens* tokens, const wb_matrix* weight, float scale, int64_t first, const wb_matrix* out,
                  void* stream);
-/* d_weight[v] = scale * sum of d_out[t] over tokens[t] - first == v, in the order
- * of t; every row of d_weight is written. `workspace`: the bytes that
+/* d_weight[v] = scale * sum of d_out[t] over tokens[t] - first == v; every row of
+ * d_weight is written. The order of the sum follows from the tokens and their count
+ * alone: the tokens sorted by row, stably, are taken in chunks of 16 to 256 (by
+ * count), a chunk's terms of a row are added by ascending t, then the chunks' sums of
+ * the row in a fixed order. The last bits of a row so go with the other tokens of the
+ * call; the same call gives the same bits. `workspace`: the bytes that
  * wb_embedding_backward_workspace gives for as many tokens and columns and rows of
  * d_weight, 16-byte aligned, free again when the call's work is done. Errors as
  * wb_embedding, and WB_ESIZE. */

@@ -3,8 +3,9 @@
 //
 // The lookup reads and writes a row per token: bandwidth bound, 16384 x 4096 bf16
 // in 32 us, 8.4 TB/s with what the caches hold of the frequent rows. The gradient sorts the
-// tokens (stable, so that a row's sum goes by ascending t and does not depend on
-// which workgroup ran first), sums runs of equal tokens, and writes every row of dW
+// tokens (stably, so that the order of a row's sum follows from the tokens and not from
+// which workgroup ran first: by ascending t within a chunk of sorted tokens, then the
+// chunks' sums), sums runs of equal tokens, and writes every row of dW
 // once, the ones without a token as zeros: 16384 tokens of 128256 in 250 us, of which
 // the sort takes 25, its four launches' latency, and what sums and writes the 1.05 GB of dW
 // 217 (the zeros alone 155 without the non-temporal hint, 180 with it; but a pass took 304 us

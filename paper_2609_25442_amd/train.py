@@ -209,7 +209,8 @@ def embedding(tokens, weight, scale=1.0, first=0, out_dtype=None, stream=None):
     (default: the weight's own).
 
     Differentiable in weight: row v's gradient is ``scale`` times the sum of the
-    results' gradients where ``tokens - first == v``, in order."""
+    results' gradients where ``tokens - first == v``, in an order that the call's
+    tokens fix."""
     if stream is not None:
         return _on(stream, lambda: embedding(tokens, weight, scale, first, out_dtype), tokens, weight)
     if _differentiated(weight):
