@@ -108,10 +108,11 @@ def route(logits, k, mask=None, renormalize=True, stream=None):
     ``E / (k n^2) * sum_e counts[e] * sum_t p[t, e]`` over the n rows routed.
 
     Returns a Routing; ``gates`` and ``loss`` are differentiable if ``logits``
-    requires a gradient, once: a second derivative raises WbError."""
+    requires a gradient, once: a second derivative raises WbError. So does a
+    capture while a graph of the same leaf, recorded on another stream, lives."""
     if stream is not None:
         return _on(stream, lambda: route(logits, k, mask, renormalize), logits, mask)
-    if getattr(logits, "requires_grad", False) and _grad_enabled():
+    if _differentiated(logits):
         return Routing(*_differentiable()(logits, k, mask, renormalize), mask, bool(renormalize))
     return Routing(*_route(logits, k, mask, renormalize), mask, bool(renormalize))
 
@@ -141,6 +142,17 @@ def _backward(logits, experts, gates, counts, routed, mask, renormalize, d_gates
 def _grad_enabled():
     _here()
     return _torch.is_grad_enabled()
+
+
+def _differentiated(*tensors):
+    """Whether a graph is being recorded that one of these is part of. torch ends the process where a capture waits for
+    another stream's graph of the same leaf: that is refused."""
+    if not any(getattr(t, "requires_grad", False) for t in tensors) or not _grad_enabled():
+        return False
+    if _torch.cuda.is_current_stream_capturing() and any(_args.held_elsewhere(t) for t in tensors if t is not None):
+        raise WbError(WB_EINVAL, "a graph recorded on another stream holds a leaf of the one being captured: drop it, "
+                                 "or capture the operator's _backward function")
+    return True
 
 
 _apply = None

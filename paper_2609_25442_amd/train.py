@@ -23,7 +23,7 @@ from __future__ import annotations
 import collections
 
 from . import DTYPES, WB_EINVAL, WB_EUNSUPPORTED, WbError, _args
-from .ops import ACTIVATIONS, _address, _grad_enabled, _here, _on, _refused, _type
+from .ops import ACTIVATIONS, _address, _differentiated, _here, _on, _refused, _type
 
 
 def _result(r):
@@ -35,18 +35,6 @@ def _code(dtype):
     import torch
 
     return {None: -1, torch.float32: 0, torch.bfloat16: 1}.get(dtype, 99)
-
-
-def _differentiated(*tensors):
-    """Whether a graph is being recorded that one of these is part of."""
-    if not any(getattr(t, "requires_grad", False) for t in tensors) or not _grad_enabled():
-        return False
-    import torch
-
-    if torch.cuda.is_current_stream_capturing() and any(_args.held_elsewhere(t) for t in tensors if t is not None):
-        raise WbError(WB_EINVAL, "a graph recorded on another stream holds a leaf of the one being captured: drop it, "
-                                 "or capture the operator's _backward function")
-    return True
 
 
 def _rows(d):
