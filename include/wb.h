@@ -724,9 +724,10 @@ int wb_add_layer_norm(const wb_matrix* x, const wb_matrix* residual, const wb_ma
  * (the gradient that total gets elsewhere) may be NULL. d_sum is written to d_x and,
  * if given, to d_residual (its own type). d_weight and d_bias, [1, cols] of WB_F32 or
  * WB_BF16, may be NULL; d_bias needs d_weight. d_x may be d_out or d_total itself, where
- * the types are alike. `workspace`: wb_add_layer_norm_backward_workspace bytes,
- * 16-byte aligned, free again when the call's work is done. Errors as
- * wb_add_layer_norm, and WB_ESIZE. */
+ * the types are alike. Rows of 8 to 8192 columns whose d_total, if any, has total's
+ * type are read once, in two launches; others twice, in three. `workspace`:
+ * wb_add_layer_norm_backward_workspace bytes, 16-byte aligned, free again when the
+ * call's work is done. Errors as wb_add_layer_norm, and WB_ESIZE. */
 int wb_add_layer_norm_backward_workspace(int64_t rows, int64_t cols, size_t* bytes);
 int wb_add_layer_norm_backward(const wb_matrix* d_out, const wb_matrix* total, const wb_matrix* weight,
                                const wb_matrix* d_total, const float* mean, const float* inv, const wb_matrix* d_x,

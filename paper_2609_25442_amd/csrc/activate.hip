@@ -6,7 +6,7 @@
 // Sixteen lanes hold the 128 columns of a scale, eight each, of both halves.
 //
 // Bandwidth bound once the instructions are few: 8192 x 28672 bf16, gated silu, in 8
-// bits: there 156 us, 6.0 TB/s, back 152, 6.3 TB/s. With a 64-bit division for a unit's row, a divided sigmoid and a divided
+// bits: there 170 us, 5.6 TB/s, back 156, 6.1 TB/s (least 156 and 150). With a 64-bit division for a unit's row, a divided sigmoid and a divided
 // scale a pass of both took 362 us, now 315.
 #include <type_traits>
 

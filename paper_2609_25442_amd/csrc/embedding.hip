@@ -2,14 +2,14 @@
 //   out_t = scale W[tok_t - first];   dW_v = scale sum_{t: tok_t - first = v} dout_t
 //
 // The lookup reads and writes a row per token: bandwidth bound, 16384 x 4096 bf16
-// in 32 us, 8.4 TB/s with what the caches hold of the frequent rows. The gradient sorts the
+// in 33 us, 8.1 TB/s with what the caches hold of the frequent rows. The gradient sorts the
 // tokens (stably, so that the order of a row's sum follows from the tokens and not from
 // which workgroup ran first: by ascending t within a chunk of sorted tokens, then the
 // chunks' sums), sums runs of equal tokens, and writes every row of dW
-// once, the ones without a token as zeros: 16384 tokens of 128256 in 250 us, of which
-// the sort takes 25, its four launches' latency, and what sums and writes the 1.05 GB of dW
-// 217 (the zeros alone 155 without the non-temporal hint, 180 with it; but a pass took 304 us
-// without, for what it left to the calls after it, and 295 with it).
+// once, the ones without a token as zeros: 16384 tokens of 128256 in 247 us, of which
+// the sort takes 24, its four launches' latency, and what sums and writes the 1.05 GB of dW
+// 217 (210 without the non-temporal hint, but then the next lookup takes 47 us, not 32, for
+// what it was left: a pass there and back on two sets of operands in turn 288 us, 277 with it).
 #include <algorithm>
 
 #include "ops_device.hpp"
@@ -292,7 +292,10 @@ __global__ __launch_bounds__(kSortThreads) void wb_sort_place_kernel(EmbedGradAr
 // the run that came in, 1: the one that goes on), which the second launch adds.
 
 constexpr int kFillRows = 32;  // at most, to a workgroup
-constexpr int kBatch = 8;  // rows under way at a time
+// Rows of a batch, their places fetched a batch ahead. Whole fp32 rows are under
+// way together; a bf16 one is widened, and so waited for, before the next is asked
+// for, inside load_eight's branch on the type.
+constexpr int kBatch = 8;
 
 struct Sorted {
   const uint32_t* keys;
@@ -447,8 +450,8 @@ __global__ __launch_bounds__(kThreads) void wb_embed_join_kernel(EmbedGradArgs a
   store_scaled(a, v, c, sum);
 }
 
-// Short chunks give few tokens more workgroups (3001 x 1499 fp32: 28 us with 16, 41 with 32), long ones leave many tokens'
-// runs fewer rows to add (16384 x 4096 with a tenth padding: the join takes 10 us with 32, 15 with 16, 25 with 8).
+// Short chunks give few tokens more workgroups (3001 x 1499 fp32: sums in 26 us with 16, 39 with 32), long ones leave many
+// tokens' runs fewer rows to add (16384 x 4096 with a tenth padding: the join takes 6 us with 32, 9 with 16, 14 with 8).
 int chunk_of(int64_t count) {
   int chunk = 16;
   while (chunk < 256 && count > int64_t(chunk) * 512) chunk *= 2;
@@ -495,8 +498,9 @@ Grids grids_of(int64_t count, int64_t rows, int64_t cols) {
   g.chunks = (count + g.chunk - 1) / g.chunk;
   const int64_t per = kThreads >> g.shift;
   g.slabs = (cols + (int64_t(8) << g.shift) - 1) / (int64_t(8) << g.shift);
-  // four rows, or as many as lie side by side: many workgroups, since each begins with a search (a pass of 512 tokens, 32000 x
-  // 4096 bf16: 66 us against 69 with eight rows and 72 with 32; 16384 of 128256: 277 against 290 and 285)
+  // four rows, or as many as lie side by side: many workgroups, since each begins with a search (passes there
+  // and back on two sets of operands in turn, 512 tokens of 32000 x 4096 bf16: 68 us against 70 with eight rows and 72 with
+  // 32; 16384 of 128256: 277 against 290 and 285)
   g.fill = static_cast<int32_t>(std::max<int64_t>(4, per));
   g.sums = (g.chunks + per - 1) / per * g.slabs, g.fills = (rows + g.fill - 1) / g.fill;
   g.joins = (cols + kJoinColumns - 1) / kJoinColumns;

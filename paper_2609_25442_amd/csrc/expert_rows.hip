@@ -6,12 +6,14 @@
 // own if tokens says so, so no two rows write one place, and counts once in a
 // row; the places that are nobody's are filled with zeros by workgroups of their own.
 //
-// Bandwidth bound: eight columns a thread, one run of them, since what hides a
-// row's way to memory here is the number of wavefronts (the gradient of 8192 x
-// 7168, k = 8: 410 us, and 560 with four runs a lane). Past the caches' size places'
-// rows are stored, and read, with the non-temporal hint, a token's own row without:
-// dispatch of the same in 183 us, 5.8 TB/s (213 with none, 220 with its row hinted too),
-// back in 177 (198 without); the gradient of the sum 4.9 TB/s, half of it written.
+// Bandwidth bound: eight columns a thread, one run of them. bf16 rows are waited
+// for one by one (load_eight widens them inside its branch on the type), so that
+// only the number of wavefronts hides a row's way to memory (the gradient of collect of
+// 8192 x 7168, k = 8: 420 us, and 560 with four runs a lane). Past the caches' size
+// places' rows are stored, and read, with the non-temporal hint, a token's own row without:
+// dispatch of the same in 182 us, 5.8 TB/s (213 with none, 220 with its row hinted too),
+// back in 179, 5.9 TB/s (198 without); the gradient of collect at 4.8 TB/s: a lane has one
+// place under way, and stores its row of d_y and fetches its gate before the next.
 #include <algorithm>
 
 #include "ops_device.hpp"
@@ -101,7 +103,7 @@ __global__ __launch_bounds__(kThreads) void wb_dispatch_kernel(DispatchArgs a, i
     if (mine[i] >= 0) store_run<NT>(static_cast<char*>(a.out) + mine[i] * a.ld_out * ob, c, a.at.cols, a.out_type, v);
 }
 
-constexpr int kBatch = 4;  // rows of a token under way at a time
+constexpr int kBatch = 4;  // rows of a token; whole fp32 ones are under way together
 
 template <bool NT>
 __global__ __launch_bounds__(kThreads) void wb_dispatch_grad_kernel(DispatchGradArgs a, int shift) {
@@ -134,7 +136,7 @@ __global__ __launch_bounds__(kThreads) void wb_dispatch_grad_kernel(DispatchGrad
 // the same terms in the same order, so the same bits over a router's places. A row
 // has one wavefront or more. Whose a place is, and whether an earlier choice has it,
 // is known while y's row is on its way (a row of y that does not count is read for
-// nothing): 8192 x 7168 of 8, bf16, in 199 us, combine 203; 333 x 1111 of 3, fp32, 4.8
+// nothing): 8192 x 7168 of 8, bf16, in 201 us, combine 203; 333 x 1111 of 3, fp32, 4.8
 // and 4.6 (5.6 with the places in LDS first).
 template <bool NT>
 __global__ __launch_bounds__(kThreads) void wb_collect_kernel(CollectArgs a, int shift) {

@@ -5,11 +5,11 @@
 //
 // Bandwidth bound. Forward, a row is held in registers between its two sums
 // (mean, then squares of what is left) and its result, as in norm.hip: 16384 x
-// 4096 bf16 with a residual in 96 us, 5.6 TB/s. Back, each operand is read once
+// 4096 bf16 with a residual in 99 us, 5.4 TB/s. Back, each operand is read once
 // too: rows pass through a workgroup that keeps the sums of dw and db of its
 // columns in registers, the next rows' loads ahead of the work on the present
-// ones, and a second launch adds the workgroups' sums: the same rows in 92 us
-// with the sums, 5.8 TB/s.
+// ones, and a second launch adds the workgroups' sums: the same rows in 96 us,
+// 5.6 TB/s, and 5 for the sums.
 #include <algorithm>
 
 #include "ops_device.hpp"
@@ -490,7 +490,7 @@ int launch_layer_norm(const LayerNormArgs& a, void* stream) {
   const int64_t runs = (a.cols + 7) / 8;
   const auto waves = [&](int v) { return static_cast<int>((runs + 64 * v - 1) / (64 * v)); };
   // Narrow rows: one wavefront each, four to a workgroup. Wider ones: two runs
-  // a lane (16384 x 4096 bf16 with a residual: 96 us against 115 of one, 105 of
+  // a lane (16384 x 4096 bf16 with a residual, at least: 96 us against 115 of one, 105 of
   // four and 123 of a wavefront a row; 512 x 7168: 9.0 us against 11.0 and 10.7),
   // past sixteen wavefronts four, past those several steps.
   if (runs <= 64) return launch<1, 4, false>(a, 1, st);
