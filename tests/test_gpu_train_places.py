@@ -141,3 +141,28 @@ def test_collect_into_the_residual_s_place_and_of_rows_that_start_anywhere():
         at = lambda v: m(*v.shape, 0, data=v.data_ptr())  # noqa: E731
         assert call("wb_collect", at(rows), p(r.positions), p(r.tokens), p(r.gates), 3, at(here), None, None, at(here), None) == 0
         assert torch.equal(here, want)
+
+
+def test_what_choices_that_do_not_count_hold_goes_nowhere():
+    """Gates and rows that are not finite, at places of no one, of others, and named again."""
+    nan, inf = float("nan"), float("inf")
+    positions = torch.tensor([[0, 0, 9, -4], [1, 3, 2, 2]])
+    tokens = torch.tensor([0, 0, 1, -1])
+    r = of(positions, tokens, torch.tensor([[2.0, nan, inf, nan], [nan, inf, 3.0, nan]]))
+    for t in ("f32", "bf16"):
+        for cols in (8, 13, 520, 2500):
+            y = torch.tensor([1.0, nan, 5.0, inf])[:, None].repeat(1, cols).to(ref.TORCH[t]).cuda()
+            assert wb.collect(y, r)[:, -1].tolist() == [2, 15] and torch.isfinite(wb.collect(y, r)).all()
+            d_y, d_g = wb.collect_backward(torch.ones(2, cols, device="cuda"), y, r)
+            assert d_y[:, -1].tolist() == [2, 0, 3, 0]
+            assert d_g.tolist() == [[cols, 0, 0, 0], [0, 0, 5 * cols, 0]]
+
+
+def test_collect_past_four_gigabytes():
+    say("collect, far rows")
+    rows, cols, k = 70000, 8192, 4
+    r = wb.route(ref.randn(rows, 8, seed=1).cuda(), k)
+    y = torch.zeros(rows * k, cols, dtype=torch.bfloat16, device="cuda")
+    y[:, 8191] = (torch.arange(rows * k, device="cuda") % 251).bfloat16()
+    out = wb.collect(y, r, gates=torch.ones(rows, k, device="cuda"), out_dtype="f32")
+    assert torch.equal(out[:, 8191], y[:, 8191].float()[r.positions.long()].sum(1)) and not out[:, :8191].any()
